@@ -370,6 +370,112 @@ bfs_status bfs_run_noalloc(const bfs_plan *plan, const void *const *dev_buffers,
  * reported.  Allocates nothing. */
 bfs_status bfs_run_status(const bfs_plan *plan, struct ihipStream_t *stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators beside the plans: what surrounds the MoE family's products and
+ * the AdamW family's step.  Plain calls without a program: the arguments are
+ * checked on the host (BFS_E_INVALID, BFS_E_RESOURCE beyond a stated limit,
+ * nothing launched), the work is enqueued on stream, nothing is allocated, no
+ * state is kept between calls, and the same inputs give the same bits in
+ * every run (no atomics on results).  Every call may be captured into a HIP
+ * graph.  The stream and the buffers belong to the current device.  Sums and
+ * softmax are in fp32, the global norm's in 64 bits; each result is rounded
+ * to its type once.
+ *
+ * Matrices are row-major with unit stride in a row and a stride between rows
+ * in elements: an output's at least the width, an input's anything from 0
+ * (one row for all).  Rows need no more than their element's alignment.
+ * Outputs must not overlap inputs or each other except where it is said.
+ */
+typedef enum { BFS_DTYPE_F32 = 0, BFS_DTYPE_BF16 = 1, BFS_DTYPE_F16 = 2 } bfs_dtype;
+
+/* Flag of the router: the weights of a token's chosen experts sum to one. */
+#define BFS_MOE_RENORMALIZE 1u
+
+/*
+ * Router: experts[t][j] (int32) the k experts of token t with the largest
+ * logits, largest first, equal ones by the lower index, and weights[t][j]
+ * (fp32) their softmax, over all experts or (BFS_MOE_RENORMALIZE) the chosen.
+ * A logit of -inf masks its expert: it is never chosen and adds nothing;
+ * where fewer than k experts are left the further slots hold -1 with weight
+ * 0.  A NaN logit ranks above all; it, or +inf, makes its token's weights
+ * NaN.  1 <= k <= min(16, n_experts), n_experts <= 1024.
+ */
+bfs_status bfs_moe_route(const void *logits, int32_t dtype, int64_t n_tokens, int32_t n_experts,
+                         int64_t logits_stride, int32_t k, uint32_t flags, int32_t *experts, float *weights,
+                         struct ihipStream_t *stream);
+
+/*
+ * Its gradient: grad_logits (of the logits' type) for the gradient of the
+ * weights, given the logits and the experts that the router chose; flags as
+ * there.  Slots whose expert is outside 0 .. n_experts - 1 add nothing; an
+ * expert named twice adds twice.
+ */
+bfs_status bfs_moe_route_grad(const void *logits, int32_t dtype, int64_t n_tokens, int32_t n_experts,
+                              int64_t logits_stride, const int32_t *experts, int32_t k, const float *grad_weights,
+                              uint32_t flags, void *grad_logits, int64_t grad_stride, struct ihipStream_t *stream);
+
+/*
+ * Dispatch: the slots (t, j) in a stable order by expert.
+ *   perm        int32 [n_tokens * k]: the token of each row, grouped by expert
+ *   expert_off  int32 [n_experts + 1]: each expert's first row; the last entry
+ *               is the number of rows
+ *   pos         int32 [n_tokens][k]: each slot's row, or -1 without an expert
+ *               (an id outside 0 .. n_experts - 1: padding)
+ *   rows        NULL with x NULL, or [n_tokens * k][width]: x[token] of each row
+ * perm and expert_off are buffers [1] and [2] of the MoE family.  Entries of
+ * perm and rows behind the last row are left as they were.  k <= 64,
+ * n_experts <= 1024, fewer than 2^31 slots.  workspace: device memory of
+ * bfs_moe_dispatch_workspace bytes (may be 0: NULL then), free to reuse when
+ * the work has completed; calls that overlap need one each.
+ */
+bfs_status bfs_moe_dispatch_workspace(int64_t n_tokens, int32_t k, int32_t n_experts, int64_t *bytes);
+bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k, int32_t n_experts, int32_t *perm,
+                            int32_t *expert_off, int32_t *pos, const void *x, int32_t dtype, int64_t width,
+                            int64_t x_stride, void *rows, int64_t rows_stride, void *workspace,
+                            int64_t workspace_bytes, struct ihipStream_t *stream);
+
+/*
+ * Combination: y[t] = sum over j of weights[t][j] * rows[pos[t][j]], in the
+ * order of j.  weights NULL: all one, which is the gradient of the dispatch
+ * (y the gradient of x).  Positions outside 0 .. n_rows - 1 add nothing; a
+ * token without a row gets zeros.  k <= 64.
+ */
+bfs_status bfs_moe_combine(const void *rows, int32_t dtype, int64_t n_rows, int64_t width, int64_t rows_stride,
+                           const int32_t *pos, const float *weights, int64_t n_tokens, int32_t k, void *y,
+                           int64_t y_stride, struct ihipStream_t *stream);
+
+/*
+ * Its gradient: grad_rows[pos[t][j]] = weights[t][j] * grad_y[t] and
+ * grad_weights[t][j] = <grad_y[t], rows[pos[t][j]]> (0 without a row).  Slots
+ * have different rows, as the dispatch gives them; rows that no slot names
+ * are left as they were.
+ */
+bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tokens, int64_t width,
+                                int64_t grad_y_stride, const void *rows, int64_t n_rows, int64_t rows_stride,
+                                const int32_t *pos, const float *weights, int32_t k, void *grad_rows,
+                                int64_t grad_rows_stride, float *grad_weights, struct ihipStream_t *stream);
+
+/*
+ * Global norm of n_tensors gradients (contiguous, numel[i] elements of
+ * dtypes[i]; host arrays, read by the call): *norm = sqrt(sum of squares), on
+ * the device.  workspace: device memory of bfs_grad_workspace bytes, aligned
+ * to 8; calls that overlap need one each.  At most 2^43 elements in all.
+ */
+bfs_status bfs_grad_workspace(int32_t n_tensors, int64_t *bytes);
+bfs_status bfs_grad_norm(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n_tensors,
+                         float *norm, void *workspace, int64_t workspace_bytes, struct ihipStream_t *stream);
+
+/*
+ * Clipping by it: outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6)).  An
+ * output has its gradient's type, and may then be the gradient itself, or is
+ * fp32 (a part of the AdamW family's flat gradient, say).  Where the norm is
+ * not finite the scale is 1.  norm: NULL, or where the norm (before clipping)
+ * goes.  max_norm >= 0.
+ */
+bfs_status bfs_grad_clip(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
+                         const int32_t *out_dtypes, int32_t n_tensors, double max_norm, float *norm, void *workspace,
+                         int64_t workspace_bytes, struct ihipStream_t *stream);
+
 const char *bfs_status_string(bfs_status s);
 const char *bfs_last_error(void);
 

@@ -25,6 +25,8 @@ KERNELS = {"interp": 0, "stream3": 1, "gemm": 2, "attn": 3, "moe": 4, "rmsnorm":
 
 EXPORTED = ["bfs_plan_create", "bfs_plan_formulas", "bfs_plan_static_waits", "bfs_plan_stats",
             "bfs_eval_threshold", "bfs_plan_destroy", "bfs_run", "bfs_run_noalloc", "bfs_run_status",
+            "bfs_moe_route", "bfs_moe_route_grad", "bfs_moe_dispatch_workspace", "bfs_moe_dispatch", "bfs_moe_combine",
+            "bfs_moe_combine_grad", "bfs_grad_workspace", "bfs_grad_norm", "bfs_grad_clip",
             "bfs_status_string", "bfs_last_error"]
 
 
@@ -101,6 +103,19 @@ def lib():
         L.bfs_run_noalloc.argtypes = L.bfs_run.argtypes
         L.bfs_run_status.restype = C.c_int
         L.bfs_run_status.argtypes = [C.c_void_p, C.c_void_p]
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        for name, args in (
+                ("bfs_moe_route", [p, i32, i64, i32, i64, i32, C.c_uint32, p, p, p]),
+                ("bfs_moe_route_grad", [p, i32, i64, i32, i64, p, i32, p, C.c_uint32, p, i64, p]),
+                ("bfs_moe_dispatch_workspace", [i64, i32, i32, C.POINTER(i64)]),
+                ("bfs_moe_dispatch", [p, i64, i32, i32, p, p, p, p, i32, i64, i64, p, i64, p, i64, p]),
+                ("bfs_moe_combine", [p, i32, i64, i64, i64, p, p, i64, i32, p, i64, p]),
+                ("bfs_moe_combine_grad", [p, i32, i64, i64, i64, p, i64, i64, p, p, i32, p, i64, p, p]),
+                ("bfs_grad_workspace", [i32, C.POINTER(i64)]),
+                ("bfs_grad_norm", [p, p, p, i32, p, p, i64, p]),
+                ("bfs_grad_clip", [p, p, p, p, p, i32, C.c_double, p, p, i64, p])):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = args
         L.bfs_status_string.restype = C.c_char_p
         L.bfs_status_string.argtypes = [C.c_int]
         L.bfs_last_error.restype = C.c_char_p

@@ -1,0 +1,143 @@
+// What the operators beside the plans share: element types, rows in 16-byte
+// chunks, reductions inside a wave and the launch call.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <string>
+
+#include "bfs_internal.h"
+
+namespace bfsop {
+
+using bfs::fail;
+
+constexpr int kWave = 64;
+
+// 16 bytes of a row.  Rows start at any element (odd widths, views), so the
+// alignment is the element's; global accesses of four words need no more.
+template <typename T>
+struct Chunk {
+  static constexpr int kElems = 16 / (int)sizeof(T);
+  typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+
+template <typename T>
+__device__ __forceinline__ T zero_of() {
+  return (T)0.0f;
+}
+
+// Elements [c * kElems, ...) of a row of n elements: a whole chunk in one
+// access, the row's last partial one by elements (zeros past the end).
+template <typename T>
+__device__ __forceinline__ typename Chunk<T>::vec load_chunk(const T *row, int64_t c, int64_t n) {
+  constexpr int E = Chunk<T>::kElems;
+  typename Chunk<T>::vec v;
+  if ((c + 1) * E <= n) {
+    v = *reinterpret_cast<const typename Chunk<T>::vec *>(row + c * E);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = c * E + i < n ? row[c * E + i] : zero_of<T>();
+  }
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_chunk(T *row, int64_t c, int64_t n, typename Chunk<T>::vec v) {
+  constexpr int E = Chunk<T>::kElems;
+  if ((c + 1) * E <= n) {
+    *reinterpret_cast<typename Chunk<T>::vec *>(row + c * E) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (c * E + i < n) row[c * E + i] = v[i];
+  }
+}
+
+// Lane i's value from lane i - s of its row of 16 lanes, the row as a ring.
+template <int s>
+__device__ __forceinline__ uint32_t ror16(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + s, 0xf, 0xf, false);
+}
+
+// Reductions over groups of G consecutive lanes (16 or 64); every lane gets
+// the same result: each step pairs values symmetrically.
+template <int G, typename F>
+__device__ __forceinline__ uint32_t group_reduce(uint32_t x, F f) {
+  static_assert(G == 16 || G == 64, "groups of 16 or 64 lanes");
+  x = f(x, ror16<8>(x));
+  x = f(x, ror16<4>(x));
+  x = f(x, ror16<2>(x));
+  x = f(x, ror16<1>(x));
+  if (G == 64) {
+    x = f(x, (uint32_t)__shfl_xor((int)x, 16));
+    x = f(x, (uint32_t)__shfl_xor((int)x, 32));
+  }
+  return x;
+}
+
+template <int G>
+__device__ __forceinline__ uint32_t group_max(uint32_t x) {
+  return group_reduce<G>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+
+template <int G>
+__device__ __forceinline__ uint32_t group_min(uint32_t x) {
+  return group_reduce<G>(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
+template <int G>
+__device__ __forceinline__ float group_maxf(float x) {
+  return __uint_as_float(group_reduce<G>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+
+template <int G>
+__device__ __forceinline__ float group_sum(float x) {
+  return __uint_as_float(group_reduce<G>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+
+// Wave index in the workgroup, in a scalar register.
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+__device__ __forceinline__ int lane_index() { return (int)(threadIdx.x & 63u); }
+
+template <typename... P, typename... A>
+bfs_status launch(const char *what, void (*kernel)(P...), int64_t blocks, int threads, size_t lds, void *stream, A... a) {
+  std::tuple<P...> params(static_cast<P>(a)...);
+  void *ptrs[sizeof...(P)];
+  std::apply([&](auto &...p) {
+    int i = 0;
+    ((ptrs[i++] = (void *)&p), ...);
+  }, params);
+  hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((uint32_t)blocks), dim3((uint32_t)threads),
+                                 ptrs, lds, (hipStream_t)stream);
+  if (e != hipSuccess) return fail(BFS_E_DEVICE, std::string(what) + ": launch: " + hipGetErrorString(e));
+  return BFS_OK;
+}
+
+// No C++ exception leaves a C entry point (the error texts allocate).
+template <typename F>
+bfs_status entry(F f) noexcept {
+  try {
+    return f();
+  } catch (...) {
+    return BFS_E_RESOURCE;
+  }
+}
+
+// f(T{}) with the element type of a bfs_dtype.
+template <typename F>
+bfs_status with_type(int32_t dtype, F f) {
+  switch (dtype) {
+    case BFS_DTYPE_F32: return f(float{});
+    case BFS_DTYPE_BF16: return f(__bf16{});
+    case BFS_DTYPE_F16: return f(_Float16{});
+    default: return fail(BFS_E_INVALID, "unknown dtype");
+  }
+}
+
+}  // namespace bfsop

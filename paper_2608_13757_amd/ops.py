@@ -1,0 +1,356 @@
+"""The operators beside the plans (include/bfs.h): a mixture of experts'
+router, dispatch and combination with their gradients, and the global gradient
+norm with clipping.
+
+Argument checks and marshalling only.  Tensors are torch tensors on the
+current device; a refused argument raises BfsError (E_INVALID or E_RESOURCE)
+before anything is launched.  Outputs that are not given are allocated on the
+current stream.  ``stream``: a torch stream or handle, None the current one;
+on another stream than the current one every output (and the workspace) has to
+be given, since an allocation belongs to the stream that it was made on.
+"""
+from __future__ import annotations
+
+import ctypes as C
+import struct
+
+import torch
+
+from . import bfs
+from .bfs import E_INVALID, OK, BfsError
+
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+MOE_RENORMALIZE = 1
+DISPATCH_ONE_LAUNCH = 1024       # slots up to which the dispatch needs no workspace
+
+
+def _refuse(name, what):
+    raise BfsError(E_INVALID, f"{name}: {what}")
+
+
+def _current_device():
+    return torch.cuda.current_device()
+
+
+def _dtype(name, t):
+    code = DTYPES.get(t.dtype)
+    if code is None:
+        _refuse(name, f"element type {t.dtype} (float32, bfloat16 and float16 are supported)")
+    return code
+
+
+def _matrix(name, what, t, device, shape=None, dtype=None, out=False):
+    """Stride between the rows of a [n, width] tensor whose rows have unit
+    stride; an output's rows must not overlap."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _refuse(name, f"{what} must be a tensor on the current device")
+    if dtype is not None and t.dtype is not dtype:
+        _refuse(name, f"{what} must be {dtype}, not {t.dtype}")
+    size = t.shape
+    if len(size) != 2 or (shape is not None and size != shape):
+        _refuse(name, f"{what} has shape {tuple(size)}, not {'two dimensions' if shape is None else tuple(shape)}")
+    n, width = size
+    stride, unit = t.stride()
+    if unit != 1 and width > 1:
+        _refuse(name, f"{what} must have unit stride in its rows")
+    if n <= 1:
+        return width
+    if out and stride < width:
+        _refuse(name, f"{what} has rows that overlap")
+    return stride
+
+
+def _dense(name, what, t, device, shape, dtype):
+    """A contiguous tensor of a given shape and type."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != device:
+        _refuse(name, f"{what} must be a tensor on the current device")
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(name, f"{what} must be contiguous {dtype} of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _stream(name, stream, given):
+    """Handle of the stream; ``given``: whether nothing has to be allocated."""
+    handle = bfs._stream_handle(stream)
+    if stream is not None and not given and handle != bfs._stream_handle(None):
+        _refuse(name, "on another stream than the current one every output and the workspace must be given")
+    return handle
+
+
+def _call(function, *args):
+    status = function(*args)
+    if status != OK:
+        bfs._check(status)
+
+
+def moe_route(logits, k, *, renormalize=True, experts=None, weights=None, stream=None):
+    """(experts int32 [T, k], weights float32 [T, k]): the k experts of each
+    token with the largest logits ([T, E]; equal ones by the lower index) and
+    their softmax over the chosen ones (``renormalize``) or over all experts.
+    A logit of -inf masks its expert; slots left without one hold -1 and
+    weight 0."""
+    name = "moe_route"
+    L = bfs._lib or bfs.lib()
+    device = _current_device()
+    stride = _matrix(name, "logits", logits, device)
+    dtype = _dtype(name, logits)
+    t, e = logits.shape
+    if k < 1:
+        _refuse(name, f"k = {k}")
+    handle = _stream(name, stream, experts is not None and weights is not None)
+    shape = (t, k)
+    if experts is None:
+        experts = logits.new_empty(shape, dtype=torch.int32)
+    else:
+        _dense(name, "experts", experts, device, shape, torch.int32)
+    if weights is None:
+        weights = logits.new_empty(shape, dtype=torch.float32)
+    else:
+        _dense(name, "weights", weights, device, shape, torch.float32)
+    _call(L.bfs_moe_route, logits.data_ptr(), dtype, t, e, stride, k, MOE_RENORMALIZE if renormalize else 0,
+          experts.data_ptr(), weights.data_ptr(), handle)
+    return experts, weights
+
+
+def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logits=None, stream=None):
+    """The gradient of the logits (of their type) for the gradient of the
+    router's weights; ``experts`` and ``renormalize`` as the router had them."""
+    name = "moe_route_grad"
+    L = bfs._lib or bfs.lib()
+    device = _current_device()
+    stride = _matrix(name, "logits", logits, device)
+    dtype = _dtype(name, logits)
+    t, e = logits.shape
+    k = experts.shape[-1]
+    _dense(name, "experts", experts, device, (t, k), torch.int32)
+    _dense(name, "grad_weights", grad_weights, device, (t, k), torch.float32)
+    handle = _stream(name, stream, grad_logits is not None)
+    if grad_logits is None:
+        grad_logits = logits.new_empty((t, e))
+    out_stride = _matrix(name, "grad_logits", grad_logits, device, logits.shape, logits.dtype, True)
+    _call(L.bfs_moe_route_grad, logits.data_ptr(), dtype, t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
+          MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride, handle)
+    return grad_logits
+
+
+def moe_dispatch_workspace(n_tokens, k, n_experts):
+    """Bytes of device memory that a dispatch of these sizes works in."""
+    n = C.c_int64()
+    _call(bfs.lib().bfs_moe_dispatch_workspace, n_tokens, k, n_experts, C.byref(n))
+    return n.value
+
+
+def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=None, rows=None, workspace=None,
+                 stream=None):
+    """(perm, expert_off, pos, rows): the slots of ``experts`` (int32 [T, k],
+    ids outside 0 .. n_experts - 1: none) in a stable order by expert.  perm
+    int32 [T * k]: each row's token; expert_off int32 [n_experts + 1]: each
+    expert's first row, last the number of rows (the MoE plans' buffers); pos
+    int32 [T, k]: each slot's row or -1; rows [T * k, width]: x[token], None
+    without x [T, width].  Entries of perm and rows behind the last row are
+    left as they were."""
+    name = "moe_dispatch"
+    L = bfs._lib or bfs.lib()
+    device = _current_device()
+    if not isinstance(experts, torch.Tensor) or experts.dim() != 2:
+        _refuse(name, "experts must be a tensor of two dimensions")
+    if n_experts < 1:
+        _refuse(name, f"n_experts = {n_experts}")
+    t, k = shape = experts.shape
+    slots = t * k
+    _dense(name, "experts", experts, device, shape, torch.int32)
+    one_launch = slots <= DISPATCH_ONE_LAUNCH
+    handle = _stream(name, stream, perm is not None and expert_off is not None and pos is not None
+                     and (x is None or rows is not None) and (one_launch or workspace is not None))
+    if perm is None:
+        perm = experts.new_empty(slots)
+    else:
+        _dense(name, "perm", perm, device, (slots,), torch.int32)
+    if expert_off is None:
+        expert_off = experts.new_empty(n_experts + 1)
+    else:
+        _dense(name, "expert_off", expert_off, device, (n_experts + 1,), torch.int32)
+    if pos is None:
+        pos = experts.new_empty(shape)
+    else:
+        _dense(name, "pos", pos, device, shape, torch.int32)
+    x_ptr = rows_ptr = None
+    dtype = width = x_stride = rows_stride = 0
+    if x is not None:
+        x_stride = _matrix(name, "x", x, device)
+        dtype = _dtype(name, x)
+        n, width = x.shape
+        if n != t:
+            _refuse(name, f"x has {n} rows for {t} tokens")
+        if rows is None:
+            rows = x.new_empty((slots, width))
+        rows_stride = _matrix(name, "rows", rows, device, (slots, width), x.dtype, True)
+        x_ptr, rows_ptr = x.data_ptr(), rows.data_ptr()
+    elif rows is not None:
+        _refuse(name, "rows without x")
+    ws_ptr, ws_bytes = None, 0
+    if not one_launch:
+        if workspace is None:
+            workspace = experts.new_empty(moe_dispatch_workspace(t, k, n_experts), dtype=torch.uint8)
+        elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != device or not workspace.is_contiguous():
+            _refuse(name, "workspace must be a contiguous tensor on the current device")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _call(L.bfs_moe_dispatch, experts.data_ptr(), t, k, n_experts, perm.data_ptr(), expert_off.data_ptr(), pos.data_ptr(),
+          x_ptr, dtype, width, x_stride, rows_ptr, rows_stride, ws_ptr, ws_bytes, handle)
+    return perm, expert_off, pos, rows
+
+
+def _combine(name, rows, pos, weights, out, stream):
+    L = bfs._lib or bfs.lib()
+    device = _current_device()
+    stride = _matrix(name, "rows", rows, device)
+    dtype = _dtype(name, rows)
+    n, width = rows.shape
+    if not isinstance(pos, torch.Tensor) or pos.dim() != 2:
+        _refuse(name, "pos must be a tensor of two dimensions")
+    t, k = shape = pos.shape
+    _dense(name, "pos", pos, device, shape, torch.int32)
+    w_ptr = None
+    if weights is not None:
+        _dense(name, "weights", weights, device, shape, torch.float32)
+        w_ptr = weights.data_ptr()
+    handle = _stream(name, stream, out is not None)
+    if out is None:
+        out = rows.new_empty((t, width))
+    out_stride = _matrix(name, "out", out, device, (t, width), rows.dtype, True)
+    _call(L.bfs_moe_combine, rows.data_ptr(), dtype, n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(),
+          out_stride, handle)
+    return out
+
+
+def moe_combine(rows, pos, weights, *, out=None, stream=None):
+    """[T, width]: the sum over j of weights[t, j] * rows[pos[t, j]]; slots
+    without a row (pos outside the rows) add nothing."""
+    if weights is None:
+        _refuse("moe_combine", "weights are needed")
+    return _combine("moe_combine", rows, pos, weights, out, stream)
+
+
+def moe_dispatch_grad(grad_rows, pos, *, out=None, stream=None):
+    """The gradient of the dispatch's x: the sum of each token's rows."""
+    return _combine("moe_dispatch_grad", grad_rows, pos, None, out, stream)
+
+
+def moe_combine_grad(grad_y, rows, pos, weights, *, grad_rows=None, grad_weights=None, stream=None):
+    """(grad_rows, grad_weights) of the combination: grad_rows[pos[t, j]] =
+    weights[t, j] * grad_y[t], grad_weights[t, j] = <grad_y[t],
+    rows[pos[t, j]]>.  Rows that no slot names are left as they were (zeros in
+    a grad_rows that the call allocates)."""
+    name = "moe_combine_grad"
+    L = bfs._lib or bfs.lib()
+    device = _current_device()
+    dy_stride = _matrix(name, "grad_y", grad_y, device)
+    dtype = _dtype(name, grad_y)
+    t, width = grad_y.shape
+    rows_stride = _matrix(name, "rows", rows, device, (rows.shape[0], width), grad_y.dtype)
+    n = rows.shape[0]
+    k = pos.shape[-1]
+    _dense(name, "pos", pos, device, (t, k), torch.int32)
+    _dense(name, "weights", weights, device, (t, k), torch.float32)
+    handle = _stream(name, stream, grad_rows is not None and grad_weights is not None)
+    if grad_rows is None:
+        grad_rows = rows.new_zeros((n, width))
+    out_stride = _matrix(name, "grad_rows", grad_rows, device, (n, width), grad_y.dtype, True)
+    if grad_weights is None:
+        grad_weights = weights.new_empty((t, k))
+    else:
+        _dense(name, "grad_weights", grad_weights, device, (t, k), torch.float32)
+    _call(L.bfs_moe_combine_grad, grad_y.data_ptr(), dtype, t, width, dy_stride, rows.data_ptr(), n, rows_stride,
+          pos.data_ptr(), weights.data_ptr(), k, grad_rows.data_ptr(), out_stride, grad_weights.data_ptr(), handle)
+    return grad_rows, grad_weights
+
+
+class GradSet:
+    """The gradients of a model, for their global norm and clipping.
+
+    ``grads``: contiguous float32, bfloat16 or float16 tensors.  ``out``: None
+    (they are clipped in place), a flat tensor that takes them one after the
+    other (float32, or the type of all of them: the gradient buffer of an
+    AdamW plan), or a tensor for each.  The set keeps the tensors' memory: a
+    gradient that is allocated anew needs a new set."""
+
+    def __init__(self, grads, out=None):
+        name = "GradSet"
+        grads = list(grads)
+        for g in grads:
+            if not isinstance(g, torch.Tensor) or not g.is_cuda or not g.is_contiguous():
+                _refuse(name, "gradients must be contiguous tensors on a device")
+        types = [_dtype(name, g) for g in grads]
+        sizes = [g.numel() for g in grads]
+        if out is None:
+            outs = grads
+        elif isinstance(out, torch.Tensor):
+            if out.dim() != 1 or out.numel() != sum(sizes) or not out.is_cuda or not out.is_contiguous():
+                _refuse(name, f"out must be a contiguous vector of {sum(sizes)} elements on a device")
+            outs = out.split(sizes) if grads else []
+        else:
+            outs = list(out)
+            if len(outs) != len(grads):
+                _refuse(name, f"{len(outs)} outputs for {len(grads)} gradients")
+            for o, g in zip(outs, grads):
+                if not isinstance(o, torch.Tensor) or not o.is_cuda or not o.is_contiguous() or o.shape != g.shape:
+                    _refuse(name, "an output must be contiguous and of its gradient's shape")
+        devices = {t.get_device() for t in [*grads, *outs]}
+        if len(devices) > 1:
+            _refuse(name, "tensors on several devices")
+        for o, g in zip(outs, grads):
+            if o.dtype is not torch.float32 and o.dtype is not g.dtype:
+                _refuse(name, f"an output is float32 or has its gradient's type, not {o.dtype} for {g.dtype}")
+        # aliases: the memory stays even where a tensor's data is exchanged
+        self._keep = [t.detach() for t in [*grads, *outs]]
+        self._device = devices.pop() if devices else None
+        self._home = grads[0].device if grads else None
+        n = self._n = len(grads)
+        self._grads = struct.pack("%dP" % n, *[g.data_ptr() for g in grads])
+        self._outs = struct.pack("%dP" % n, *[o.data_ptr() for o in outs])
+        self._sizes = struct.pack("%dq" % n, *sizes)
+        self._types = struct.pack("%di" % n, *types)
+        self._out_types = struct.pack("%di" % n, *[DTYPES[o.dtype] for o in outs])
+        bytes_ = C.c_int64()
+        _call(bfs.lib().bfs_grad_workspace, n, C.byref(bytes_))
+        self.workspace_bytes = bytes_.value
+
+    def _buffers(self, name, norm, workspace, stream):
+        device = _current_device()
+        if self._device is not None and device != self._device:
+            _refuse(name, "the gradients are not on the current device")
+        handle = _stream(name, stream, norm is not None and workspace is not None)
+        if norm is None:
+            norm = torch.empty((), dtype=torch.float32, device="cuda")
+        else:
+            _dense(name, "norm", norm, device, (), torch.float32)
+        if workspace is None:
+            workspace = norm.new_empty(self.workspace_bytes, dtype=torch.uint8)
+        elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != device or not workspace.is_contiguous():
+            _refuse(name, "workspace must be a contiguous tensor on the current device")
+        return norm, workspace, workspace.numel() * workspace.element_size(), handle
+
+    def norm(self, norm=None, workspace=None, stream=None):
+        """The global norm, a float32 scalar on the device."""
+        norm, workspace, size, handle = self._buffers("grad_norm", norm, workspace, stream)
+        _call(bfs.lib().bfs_grad_norm, self._grads, self._sizes, self._types, self._n, norm.data_ptr(),
+              workspace.data_ptr(), size, handle)
+        return norm
+
+    def clip(self, max_norm, norm=None, workspace=None, stream=None):
+        """Writes grads * min(1, max_norm / (norm + 1e-6)) to the outputs and
+        returns the norm before clipping.  A norm that is not finite scales by
+        1."""
+        norm, workspace, size, handle = self._buffers("grad_clip", norm, workspace, stream)
+        _call(bfs.lib().bfs_grad_clip, self._grads, self._outs, self._sizes, self._types, self._out_types, self._n, max_norm,
+              norm.data_ptr(), workspace.data_ptr(), size, handle)
+        return norm
+
+
+def grad_norm(grads, **kw):
+    """GradSet(grads).norm(), for gradients that are used once."""
+    return GradSet(grads).norm(**kw)
+
+
+def grad_clip(grads, max_norm, out=None, **kw):
+    """GradSet(grads, out).clip(max_norm), for gradients that are used once."""
+    return GradSet(grads, out).clip(max_norm, **kw)

@@ -1,0 +1,143 @@
+"""The global gradient norm and clipping against their definition in 64 bits.
+
+Bounds (u = 2^-24, h half a step of the output's type): the squares of fp32
+values are exact to 2^-53 and summed in 64 bits, so the norm is off by its one
+rounding to fp32, u, and n 2^-52 of the sum; the scale is rounded once (u) and
+so is the product (u, then h for a 16-bit output)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2608_13757_amd as bfsp  # noqa: E402
+from paper_2608_13757_amd import BfsError, GradSet, bfs  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DTYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    bfs.lib()
+
+
+def _grads(seed, sizes, dtypes, scale=0.01):
+    g = torch.Generator().manual_seed(seed)
+    return [(torch.randn(n, generator=g) * scale).to(dtypes[i % len(dtypes)]).cuda() for i, n in enumerate(sizes)]
+
+
+def _norm64(grads):
+    return float(np.sqrt(sum((g.double().cpu().numpy() ** 2).sum() for g in grads)))
+
+
+def _check_norm(got, grads):
+    ref, n = _norm64(grads), sum(g.numel() for g in grads)
+    assert got.shape == () and got.dtype == torch.float32
+    assert abs(float(got) - ref) <= ref * (U + n * 2.0 ** -52) * 1.001, (float(got), ref)
+    return ref
+
+
+def _check_out(out, g, scale, dtype):
+    fi, ref = torch.finfo(dtype), g.double().cpu().numpy().reshape(-1) * scale
+    allowed = np.abs(ref) * (3 * U + fi.eps / 2 * (1 + 3 * U)) + fi.tiny * fi.eps / 2 + 2.0 ** -150
+    err = np.abs(out.double().cpu().numpy().reshape(-1) - ref)
+    assert (err <= allowed).all(), err.max()
+
+
+SIZES = [[1], [7], [4096], [8191, 1, 8193], [5, 0, 100000, 3, 0, 16384], [1] * 200, [300 * i + 1 for i in range(140)],
+         [3_000_001, 17, 64]]
+
+
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: f"{len(s)}x{max(s)}")
+@pytest.mark.parametrize("dtypes", [DTYPES[:1], DTYPES[1:2], DTYPES], ids=["fp32", "bf16", "mixed"])
+@pytest.mark.parametrize("max_norm", [0.05, 1e9])
+def test_norm_and_clip(sizes, dtypes, max_norm):
+    grads = _grads(len(sizes), sizes, dtypes)
+    ref = _check_norm(GradSet(grads).norm(), grads)
+    scale = min(1.0, max_norm / (ref + 1e-6))
+    # into a flat fp32 vector, between sentinels and off any alignment
+    buf = torch.full((sum(sizes) + 8,), 77.0, device="cuda")
+    flat = buf[3:3 + sum(sizes)]
+    norm = GradSet(grads, out=flat).clip(max_norm)
+    _check_norm(norm, grads)
+    assert (buf[:3] == 77).all() and (buf[3 + sum(sizes):] == 77).all()
+    for o, g in zip(flat.split(sizes), grads):
+        _check_out(o, g, scale, torch.float32)
+    # a tensor for each, of the gradients' type, then in place: the same bits
+    outs = [torch.full_like(g, 5) for g in grads]
+    GradSet(grads, out=outs).clip(max_norm)
+    for o, g in zip(outs, grads):
+        _check_out(o, g, scale, g.dtype)
+    norm2 = GradSet(grads).clip(max_norm)
+    assert torch.equal(norm, norm2) and all(torch.equal(o, g) for o, g in zip(outs, grads))
+
+
+def test_same_bits_every_run_and_one_shot_calls():
+    grads = _grads(3, [100003, 5000, 77], DTYPES, 1.0)
+    s = GradSet(grads)
+    first = s.norm()
+    for _ in range(5):
+        assert torch.equal(s.norm(), first)
+    assert torch.equal(bfsp.grad_norm(grads), first)
+    want = [(g.float() * float(np.float32(2.0 / (_norm64(grads) + 1e-6)))).to(g.dtype) for g in grads]
+    assert torch.equal(bfsp.grad_clip(grads, 2.0), first)
+    for g, w in zip(grads, want):
+        assert (g.float() - w.float()).abs().max() <= torch.finfo(g.dtype).eps * w.float().abs().max()
+
+
+@pytest.mark.parametrize("dtype,big", [(torch.float32, 1e30), (torch.bfloat16, 1e30), (torch.float32, 1e-30)])
+def test_squares_outside_fp32(dtype, big):
+    """Squares beyond fp32's range (or below it) do not spoil the norm."""
+    grads = [(torch.randn(1000, generator=torch.Generator().manual_seed(4)) * big).to(dtype).cuda()]
+    ref = _check_norm(GradSet(grads).norm(), grads)
+    out = torch.empty(1000, device="cuda")
+    GradSet(grads, out=out).clip(0.5)
+    _check_out(out, grads[0], min(1.0, 0.5 / (ref + 1e-6)), torch.float32)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_norm_not_finite(bad):
+    """The norm says so; the gradients stay as they are, in place or copied."""
+    grads = _grads(5, [100, 9000], [torch.float32])
+    grads[1][8500] = bad
+    before = [g.clone() for g in grads]
+    out = torch.empty(9100, device="cuda")
+    norm = GradSet(grads, out=out).clip(0.01)
+    assert norm.isnan() if bad != bad else norm == float("inf")
+    assert torch.equal(torch.nan_to_num(out), torch.nan_to_num(torch.cat(before)))
+    GradSet(grads).clip(0.01)
+    assert all(torch.equal(torch.nan_to_num(a), torch.nan_to_num(b)) for a, b in zip(grads, before))
+
+
+def test_zeros_empty_and_max_norm_zero():
+    assert GradSet([]).norm() == 0 and GradSet([]).clip(1.0) == 0
+    empty = [torch.empty(0, device="cuda"), torch.empty((3, 0), device="cuda")]
+    assert GradSet(empty).norm() == 0 and GradSet(empty).clip(1.0) == 0
+    zeros = [torch.zeros(100, device="cuda")]
+    assert GradSet(zeros).clip(1.0) == 0 and (zeros[0] == 0).all()
+    g = _grads(6, [50], [torch.float32])
+    assert GradSet(g).clip(0.0) > 0 and (g[0] == 0).all()
+
+
+def test_shared_gradient_counts_twice_in_the_norm():
+    """The same tensor named twice adds twice to the norm (out of place)."""
+    g = _grads(7, [500], [torch.float32])[0]
+    assert abs(float(GradSet([g, g]).norm()) - 2 ** 0.5 * _norm64([g])) <= 4 * U * _norm64([g])
+
+
+def test_refusals():
+    g = torch.zeros(8, device="cuda")
+    for call in (lambda: GradSet([g.cpu()]), lambda: GradSet([g[::2]]), lambda: GradSet([g.int()]),
+                 lambda: GradSet([g], out=torch.empty(7, device="cuda")), lambda: GradSet([g], out=torch.empty(8)),
+                 lambda: GradSet([g], out=g.half()), lambda: GradSet([g], out=[]), lambda: GradSet([g], out=[g[:4]]),
+                 lambda: GradSet([g.half()], out=[g.bfloat16()]), lambda: GradSet([g]).clip(-1.0),
+                 lambda: GradSet([g]).clip(float("nan")), lambda: GradSet([g]).norm(norm=torch.empty(1, device="cuda")),
+                 lambda: GradSet([g]).norm(workspace=torch.empty(8, device="cuda")),
+                 lambda: GradSet([g]).norm(stream=torch.cuda.Stream())):
+        with pytest.raises(BfsError) as e:
+            call()
+        assert e.value.status == bfs.E_INVALID

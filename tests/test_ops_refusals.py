@@ -1,0 +1,131 @@
+"""Refusals of the operators beside the plans, on the host: every call here
+returns an error (or has nothing to do) before anything would be launched, so
+the addresses are never used."""
+import ctypes as C
+import subprocess
+import sys
+
+import pytest
+
+from paper_2608_13757_amd import BfsError, bfs
+
+A = 1 << 20                     # an address that no call uses
+F32, BF16, F16 = 0, 1, 2
+
+
+def _status(name, *args):
+    return getattr(bfs.lib(), name)(*args)
+
+
+def _route(logits=A, dtype=F32, t=4, e=8, stride=8, k=2, flags=1, experts=A, weights=A):
+    return _status("bfs_moe_route", logits, dtype, t, e, stride, k, flags, experts, weights, None)
+
+
+def _route_grad(logits=A, dtype=F32, t=4, e=8, stride=8, experts=A, k=2, dw=A, flags=1, out=A, out_stride=8):
+    return _status("bfs_moe_route_grad", logits, dtype, t, e, stride, experts, k, dw, flags, out, out_stride, None)
+
+
+def _dispatch(experts=A, t=4, k=2, e=8, perm=A, off=A, pos=A, x=A, dtype=BF16, width=16, x_stride=16, rows=A,
+              rows_stride=16, ws=None, ws_bytes=0):
+    return _status("bfs_moe_dispatch", experts, t, k, e, perm, off, pos, x, dtype, width, x_stride, rows, rows_stride, ws,
+                   ws_bytes, None)
+
+
+def _combine(rows=A, dtype=BF16, n=8, width=16, stride=16, pos=A, w=A, t=4, k=2, y=A, y_stride=16):
+    return _status("bfs_moe_combine", rows, dtype, n, width, stride, pos, w, t, k, y, y_stride, None)
+
+
+def _combine_grad(dy=A, dtype=BF16, t=4, width=16, dy_stride=16, rows=A, n=8, stride=16, pos=A, w=A, k=2, out=A,
+                  out_stride=16, dw=A):
+    return _status("bfs_moe_combine_grad", dy, dtype, t, width, dy_stride, rows, n, stride, pos, w, k, out, out_stride, dw,
+                   None)
+
+
+def _list(values, kind):
+    return (kind * max(1, len(values)))(*values)
+
+
+def _norm(grads=(A,), numel=(4,), dtypes=(F32,), n=None, norm=A, ws=A, ws_bytes=1 << 20):
+    return _status("bfs_grad_norm", _list(grads, C.c_void_p), _list(numel, C.c_int64), _list(dtypes, C.c_int32),
+                   len(grads) if n is None else n, norm, ws, ws_bytes, None)
+
+
+def _clip(grads=(A,), outs=(A,), numel=(4,), dtypes=(F32,), out_dtypes=(F32,), max_norm=1.0, ws=A, ws_bytes=1 << 20):
+    return _status("bfs_grad_clip", _list(grads, C.c_void_p), _list(outs, C.c_void_p), _list(numel, C.c_int64),
+                   _list(dtypes, C.c_int32), _list(out_dtypes, C.c_int32), len(grads), max_norm, A, ws, ws_bytes, None)
+
+
+INVALID = [
+    (_route, dict(t=-1)), (_route, dict(e=0)), (_route, dict(k=0)), (_route, dict(k=9)), (_route, dict(stride=-1)),
+    (_route, dict(flags=2)), (_route, dict(dtype=3)), (_route, dict(dtype=-1)), (_route, dict(logits=None)),
+    (_route, dict(experts=None)), (_route, dict(weights=None)),
+    (_route_grad, dict(out_stride=7)), (_route_grad, dict(stride=-8)), (_route_grad, dict(k=9)),
+    (_route_grad, dict(experts=None)), (_route_grad, dict(dw=None)), (_route_grad, dict(out=None)),
+    (_route_grad, dict(flags=8)), (_route_grad, dict(dtype=7)),
+    (_dispatch, dict(t=-1)), (_dispatch, dict(k=0)), (_dispatch, dict(e=0)), (_dispatch, dict(experts=None)),
+    (_dispatch, dict(perm=None)), (_dispatch, dict(off=None)), (_dispatch, dict(pos=None)), (_dispatch, dict(x=None)),
+    (_dispatch, dict(rows=None)), (_dispatch, dict(width=-1)), (_dispatch, dict(rows_stride=15)),
+    (_dispatch, dict(x_stride=-16)), (_dispatch, dict(dtype=3)), (_dispatch, dict(t=4096)),
+    (_dispatch, dict(t=4096, ws=A, ws_bytes=4)), (_dispatch, dict(t=4096, ws=A + 2, ws_bytes=1 << 20)),
+    (_combine, dict(n=-1)), (_combine, dict(width=-1)), (_combine, dict(t=-1)), (_combine, dict(k=0)),
+    (_combine, dict(stride=-1)), (_combine, dict(y_stride=15)), (_combine, dict(dtype=3)), (_combine, dict(pos=None)),
+    (_combine, dict(y=None)), (_combine, dict(rows=None)),
+    (_combine_grad, dict(out_stride=15)), (_combine_grad, dict(dy_stride=-1)), (_combine_grad, dict(stride=-1)),
+    (_combine_grad, dict(w=None)), (_combine_grad, dict(dw=None)), (_combine_grad, dict(dy=None)),
+    (_combine_grad, dict(rows=None)), (_combine_grad, dict(out=None)), (_combine_grad, dict(dtype=5)),
+    (_norm, dict(n=-1)), (_norm, dict(numel=(-4,))), (_norm, dict(grads=(None,))), (_norm, dict(dtypes=(3,))),
+    (_norm, dict(norm=None)), (_norm, dict(ws=None)), (_norm, dict(ws_bytes=64)), (_norm, dict(ws=A + 4)),
+    (_clip, dict(max_norm=-1.0)), (_clip, dict(max_norm=float("nan"))), (_clip, dict(outs=(None,))),
+    (_clip, dict(out_dtypes=(BF16,))), (_clip, dict(dtypes=(BF16,), out_dtypes=(F16,))), (_clip, dict(out_dtypes=(9,))),
+    (_clip, dict(ws=None)), (_clip, dict(ws_bytes=0)),
+]
+
+
+@pytest.mark.parametrize("call,kw", INVALID, ids=lambda v: getattr(v, "__name__", str(v)))
+def test_invalid_arguments(call, kw):
+    assert call(**kw) == bfs.E_INVALID
+    assert bfs.lib().bfs_last_error()
+
+
+RESOURCE = [(_route, dict(e=1025, stride=1025)), (_route, dict(e=64, stride=64, k=17)), (_route, dict(t=1 << 31)),
+            (_dispatch, dict(e=1025)), (_dispatch, dict(k=65)), (_dispatch, dict(t=1 << 30)), (_combine, dict(k=65)),
+            (_combine, dict(t=1 << 30)), (_combine, dict(n=1 << 31)), (_combine_grad, dict(t=1 << 30)),
+            (_norm, dict(numel=(1 << 44,))), (_norm, dict(grads=(A, A), numel=(1 << 42, 1 << 43), dtypes=(F32, F32)))]
+
+
+@pytest.mark.parametrize("call,kw", RESOURCE, ids=lambda v: getattr(v, "__name__", str(v)))
+def test_beyond_the_limits(call, kw):
+    assert call(**kw) == bfs.E_RESOURCE
+
+
+def test_nothing_to_do():
+    """No tokens, or no width: done without a buffer."""
+    assert _route(t=0, logits=None, experts=None, weights=None) == bfs.OK
+    assert _route_grad(t=0, logits=None, experts=None, dw=None, out=None) == bfs.OK
+    assert _combine(t=0, rows=None, n=0, pos=None, w=None, y=None) == bfs.OK
+    assert _combine(width=0, stride=0, y_stride=0, rows=None, y=None) == bfs.OK
+    assert _combine_grad(t=0, dy=None, rows=None, n=0, pos=None, w=None, out=None, dw=None) == bfs.OK
+
+
+def test_workspaces():
+    torch = pytest.importorskip("torch")
+    from paper_2608_13757_amd import GradSet, moe_dispatch_workspace
+    assert moe_dispatch_workspace(1, 1, 64) == 0
+    assert moe_dispatch_workspace(32768, 2, 64) > 0
+    for bad in ((-1, 1, 4), (4, 0, 4), (4, 1, 0)):
+        with pytest.raises(BfsError) as e:
+            moe_dispatch_workspace(*bad)
+        assert e.value.status == bfs.E_INVALID
+    n = C.c_int64()
+    assert _status("bfs_grad_workspace", -1, C.byref(n)) == bfs.E_INVALID
+    assert _status("bfs_grad_workspace", 3, None) == bfs.E_INVALID
+    assert _status("bfs_grad_workspace", 0, C.byref(n)) == bfs.OK and n.value > 0
+    with pytest.raises(BfsError):
+        GradSet([torch.zeros(3)])                     # not on a device
+
+
+def test_package_imports_without_the_operators():
+    """The operators are loaded at their first use: the binding alone needs no torch."""
+    code = ("import sys; import paper_2608_13757_amd as p; assert 'torch' not in sys.modules; p.lib(); "
+            "assert 'torch' not in sys.modules\ntry:\n p.no_such_name\nexcept AttributeError: pass\nelse: raise SystemExit(1)")
+    subprocess.run([sys.executable, "-c", code], check=True)
