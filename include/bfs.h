@@ -456,24 +456,42 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
                                 int64_t grad_rows_stride, float *grad_weights, struct ihipStream_t *stream);
 
 /*
- * Global norm of n_tensors gradients (contiguous, numel[i] elements of
- * dtypes[i]; host arrays, read by the call): *norm = sqrt(sum of squares), on
- * the device.  workspace: device memory of bfs_grad_workspace bytes, aligned
- * to 8; calls that overlap need one each.  At most 2^43 elements in all.
+ * The gradients of a model, for their global norm and clipping.  A set is made
+ * once for n_tensors contiguous tensors (host arrays: addresses, numel[i]
+ * elements of dtypes[i]) and their outputs: each has its gradient's type, and
+ * may then be the gradient itself, or is fp32 (a part of the AdamW family's
+ * flat gradient, say).  bfs_grad_table fills *set and, where image is given,
+ * writes the table of set->image_bytes bytes to it (host memory; call once
+ * with NULL for the size).  The caller lays the table into device memory
+ * (aligned to 16 bytes), which, like the tensors, must stay as it is while
+ * calls use it.  The calls read *set and change nothing in it.  At most 2^43
+ * elements in all.
  */
-bfs_status bfs_grad_workspace(int32_t n_tensors, int64_t *bytes);
-bfs_status bfs_grad_norm(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n_tensors,
-                         float *norm, void *workspace, int64_t workspace_bytes, struct ihipStream_t *stream);
+typedef struct {
+  int64_t image_bytes;           /* device memory of the table */
+  int64_t workspace_bytes;       /* device memory that a call works in */
+  int64_t chunk;                 /* the launches' shape, the library's own */
+  int32_t n_entries, n_chunks, n_blocks, reserved;
+} bfs_grad_set;
+
+bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
+                          const int32_t *out_dtypes, int32_t n_tensors, bfs_grad_set *set, void *image,
+                          int64_t image_bytes);
 
 /*
- * Clipping by it: outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6)).  An
- * output has its gradient's type, and may then be the gradient itself, or is
- * fp32 (a part of the AdamW family's flat gradient, say).  Where the norm is
+ * *norm = sqrt(sum of squares over all gradients), on the device.  workspace:
+ * device memory of set->workspace_bytes, aligned to 8; calls that overlap need
+ * one each.
+ */
+bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *norm, void *workspace,
+                         int64_t workspace_bytes, struct ihipStream_t *stream);
+
+/*
+ * outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6)).  Where the norm is
  * not finite the scale is 1.  norm: NULL, or where the norm (before clipping)
  * goes.  max_norm >= 0.
  */
-bfs_status bfs_grad_clip(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
-                         const int32_t *out_dtypes, int32_t n_tensors, double max_norm, float *norm, void *workspace,
+bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double max_norm, float *norm, void *workspace,
                          int64_t workspace_bytes, struct ihipStream_t *stream);
 
 const char *bfs_status_string(bfs_status s);

@@ -12,10 +12,16 @@
 //
 // Two passes over the gradients, since the scale depends on all of them;
 // bound by memory.  The second goes over the chunks in the opposite order, so
-// that it begins with what the 256 MiB last-level cache still holds.  Pointers
-// and sizes travel in the launch's arguments, kTensors per launch: no table
-// to upload, nothing kept between calls.
+// that it begins with what the 256 MiB last-level cache still holds.  The
+// tensors' table is made on the host and laid into device memory by the
+// caller, once for a set of tensors: one launch for each pass whatever their
+// number (as launch arguments, 128 tensors a launch, 2^28 bf16 gradients in 290
+// tensors took six launches and 510 us).
+//
+// 2^28 bf16 gradients in 290 tensors into fp32: 405 us, 5.3 TB/s over both
+// passes, a large copy's rate; 2^20 fp32 in 24: 9 us, two short launches.
 #include <cmath>
+#include <cstring>
 #include <tuple>
 
 #include "op_common.h"
@@ -24,34 +30,40 @@ using namespace bfsop;
 
 namespace {
 
-constexpr int kTensors = 128;
 constexpr int kThreads = 256;
-constexpr int64_t kChunk = 8192;                  // elements a workgroup takes at once
-constexpr int kBlocks = 2048;                     // workgroups of all launches of a call
+constexpr int kUnroll = 8;                        // accesses of a lane in flight
+// Elements a workgroup takes at once, less where the tensors would leave
+// workgroups idle (2^28 bf16 in 290 tensors: 405 us with 8192, 416 with 16384,
+// whose last chunks are less even over the workgroups, 427 with 4096).
+constexpr int64_t kMaxChunk = 8192, kMinChunk = 2048;
+constexpr int kBlocks = 1024;                     // workgroups at most (2048: 425 us there)
+constexpr int kLine = 128;                        // bytes of a cache line
+constexpr int64_t kMaxElements = (int64_t)1 << 43;
 constexpr double kEps = 1e-6;
 
-struct TensorList {
-  const void *in[kTensors];
-  void *out[kTensors];
-  int64_t n[kTensors];
-  int32_t first[kTensors];       // the tensor's first chunk
-  uint8_t type[kTensors];        // bfs_dtype of in | of out << 4
-  int32_t n_tensors, n_chunks;
+// A tensor of the table: its chunks are first .. first + chunks - 1 of all.
+struct Entry {
+  const void *in;
+  void *out;
+  int64_t n;
+  int32_t first, chunks;
+  int32_t type;                  // bfs_dtype of in | of out << 4
+  int32_t pad;
 };
-static_assert(sizeof(TensorList) <= 4000, "launch arguments");
 
-// The tensor that holds chunk c.
-__device__ __forceinline__ int tensor_of(const TensorList &L, int c) {
-  int lo = 0, hi = L.n_tensors - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (L.first[mid] <= c) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
+// The table in device memory: the entries, then the entry that holds each
+// workgroup's first chunk.
+struct Table {
+  const Entry *entry;
+  const int32_t *start;
+  int64_t chunk;
+  int32_t n_chunks;
+};
 
-// Sum of s over the workgroup, in a fixed order, in thread 0.
+// Workgroup b of n runs chunks from .. to - 1.
+__device__ __forceinline__ int first_chunk(const Table &t, int b) { return (int)((int64_t)t.n_chunks * b / gridDim.x); }
+
+// Sum of s over the workgroup, in a fixed order, for every thread.
 __device__ __forceinline__ double block_sum(double s) {
   __shared__ double part[kThreads / kWave];
 #pragma unroll
@@ -65,30 +77,72 @@ __device__ __forceinline__ double block_sum(double s) {
   return t;
 }
 
+// Elements before the first whole line at p.
 template <typename T>
-__device__ __forceinline__ double square_sum(const T *g, int64_t n) {
-  double s = 0.0;
-  const int64_t chunks = (n + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
-  for (int64_t c = threadIdx.x; c < chunks; c += kThreads) {
-    const auto v = load_chunk<T>(g, c, n);
+__device__ __forceinline__ int head_of(const T *p, int64_t n) {
+  const int h = (int)((kLine - (uintptr_t)p % kLine) % kLine / sizeof(T));
+  return h < n ? h : (int)n;
+}
+
+// f on this lane's vectors while U accesses are whole, then with U / 2 of them.
+template <int U, typename Vec, int V, typename T, typename F>
+__device__ __forceinline__ void each_vector(const T *g, int64_t at, int64_t end, F f) {
+  constexpr int kStep = kThreads * V;
+  while (at + (U - 1) * kStep < end) {
+    Vec v[U];
 #pragma unroll
-    for (int i = 0; i < Chunk<T>::kElems; ++i) s += (double)(float)v[i] * (double)(float)v[i];
+    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec *>(g + at + u * kStep);
+#pragma unroll
+    for (int u = 0; u < U; ++u) f(at + u * kStep, v[u]);
+    at += U * kStep;
+    if (U < kUnroll) break;                       // fewer than U accesses are left
   }
+  if constexpr (U > 1) each_vector<U / 2, Vec, V>(g, at, end, f);
+}
+
+// Chunk c of a tensor of n elements at g, `chunks` of them in all, whose first
+// whole line (of `aligned`: g itself or the output) begins at element head:
+// chunks begin with a line, the first one at element 0, the last one takes
+// what is left.  f(first element, vector) for this lane's vectors, up to
+// kUnroll accesses issued before the first is used, one(element) for the
+// elements that no vector holds.
+template <typename Vec, int V, typename T, typename F, typename One>
+__device__ __forceinline__ void each_element(const T *g, int64_t n, int head, int64_t chunk, int c, int chunks, F f, One one) {
+  const int64_t from = head + c * chunk, to = c + 1 == chunks || from + chunk > n ? n : from + chunk;
+  if (c == 0 && (int)threadIdx.x < head) one((int64_t)threadIdx.x);
+  if (from >= to) return;
+  const int64_t end = to - (to - from) % V;
+  each_vector<kUnroll, Vec, V>(g, from + (int64_t)threadIdx.x * V, end, f);
+  if (end + threadIdx.x < to) one(end + threadIdx.x);
+}
+
+template <typename T>
+__device__ __forceinline__ double square_sum(const Entry &e, int64_t chunk, int c) {
+  constexpr int V = Chunk<T>::kElems;
+  typedef typename Chunk<T>::vec vec;
+  const T *g = static_cast<const T *>(e.in);
+  double s = 0.0;
+  each_element<vec, V>(
+      g, e.n, head_of(g, e.n), chunk, c, e.chunks,
+      [&](int64_t, vec v) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) s += (double)(float)v[i] * (double)(float)v[i];
+      },
+      [&](int64_t i) { s += (double)(float)g[i] * (double)(float)g[i]; });
   return s;
 }
 
-__global__ void __launch_bounds__(kThreads) square_kernel(TensorList L, double *partial) {
-  const int from = (int)((int64_t)L.n_chunks * blockIdx.x / gridDim.x);
-  const int to = (int)((int64_t)L.n_chunks * (blockIdx.x + 1) / gridDim.x);
+__global__ void __launch_bounds__(kThreads) square_kernel(Table t, double *partial) {
+  const int from = first_chunk(t, (int)blockIdx.x), to = first_chunk(t, (int)blockIdx.x + 1);
   double s = 0.0;
-  int i = tensor_of(L, from);
+  int i = t.start[blockIdx.x];
   for (int c = from; c < to; ++c) {
-    while (i + 1 < L.n_tensors && L.first[i + 1] <= c) ++i;
-    const int64_t at = (int64_t)(c - L.first[i]) * kChunk, left = L.n[i] - at, n = left < kChunk ? left : kChunk;
-    switch (L.type[i] & 15) {
-      case BFS_DTYPE_F32: s += square_sum(static_cast<const float *>(L.in[i]) + at, n); break;
-      case BFS_DTYPE_BF16: s += square_sum(static_cast<const __bf16 *>(L.in[i]) + at, n); break;
-      default: s += square_sum(static_cast<const _Float16 *>(L.in[i]) + at, n); break;
+    while (t.entry[i].first + t.entry[i].chunks <= c) ++i;
+    const Entry e = t.entry[i];
+    switch (e.type & 15) {
+      case BFS_DTYPE_F32: s += square_sum<float>(e, t.chunk, c - e.first); break;
+      case BFS_DTYPE_BF16: s += square_sum<__bf16>(e, t.chunk, c - e.first); break;
+      default: s += square_sum<_Float16>(e, t.chunk, c - e.first); break;
     }
   }
   s = block_sum(s);
@@ -106,111 +160,71 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double *partial, i
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
+// A lane's access is 16 bytes of the output, where the chunks begin with a
+// line: into a flat vector, in which tensors begin anywhere, whole lines are
+// written.  Nontemporal stores leave the last-level cache to the gradients that
+// the pass is still to read (2^25 fp32: 64 us with plain stores, 45 with these;
+// 2^23 and below: the same).
 template <typename T, typename U>
-__device__ __forceinline__ void scale_chunk(const T *g, U *out, int64_t n, float scale) {
-  constexpr int E = Chunk<T>::kElems;
-  typedef U vec __attribute__((ext_vector_type(E), aligned(sizeof(U))));
-  const int64_t chunks = (n + E - 1) / E;
-  for (int64_t c = threadIdx.x; c < chunks; c += kThreads) {
-    const auto v = load_chunk<T>(g, c, n);
-    vec o;
+__device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c, float scale) {
+  constexpr int V = Chunk<U>::kElems;
+  typedef T in_vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  typedef typename Chunk<U>::vec vec;
+  const T *g = static_cast<const T *>(e.in);
+  U *out = static_cast<U *>(e.out);
+  each_element<in_vec, V>(
+      g, e.n, head_of(out, e.n), chunk, c, e.chunks,
+      [&](int64_t i, in_vec v) {
+        vec o;
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = (U)((float)v[i] * scale);
-    if ((c + 1) * E <= n) {
-      *reinterpret_cast<vec *>(out + c * E) = o;
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (c * E + i < n) out[c * E + i] = o[i];
-    }
-  }
+        for (int j = 0; j < V; ++j) o[j] = (U)((float)v[j] * scale);
+        __builtin_nontemporal_store(o, reinterpret_cast<vec *>(out + i));
+      },
+      [&](int64_t i) { out[i] = (U)((float)g[i] * scale); });
 }
 
-__global__ void __launch_bounds__(kThreads) clip_kernel(TensorList L, const double *partial, int n_partial, double max_norm,
-                                                        float *norm) {
-  const double total = total_of(partial, n_partial), root = sqrt(total);
+__global__ void __launch_bounds__(kThreads) clip_kernel(Table t, const double *partial, double max_norm, float *norm) {
+  const double root = sqrt(total_of(partial, (int)gridDim.x));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
   const double ratio = max_norm / (root + kEps);
   const float scale = isfinite(root) && ratio < 1.0 ? (float)ratio : 1.0f;
   const int back = (int)(gridDim.x - 1 - blockIdx.x);
-  const int from = (int)((int64_t)L.n_chunks * back / gridDim.x);
-  const int to = (int)((int64_t)L.n_chunks * (back + 1) / gridDim.x);
-  int i = tensor_of(L, to - 1);
+  const int from = first_chunk(t, back), to = first_chunk(t, back + 1);
+  int i = t.start[back];
+  while (t.entry[i].first + t.entry[i].chunks < to) ++i;
   for (int c = to - 1; c >= from; --c) {
-    while (L.first[i] > c) --i;
-    if (scale == 1.0f && L.in[i] == L.out[i]) continue;
-    const int64_t at = (int64_t)(c - L.first[i]) * kChunk, left = L.n[i] - at, n = left < kChunk ? left : kChunk;
-    const void *in = L.in[i];
-    void *out = L.out[i];
-    switch (L.type[i]) {
-      case BFS_DTYPE_F32: scale_chunk(static_cast<const float *>(in) + at, static_cast<float *>(out) + at, n, scale); break;
-      case BFS_DTYPE_BF16: scale_chunk(static_cast<const __bf16 *>(in) + at, static_cast<float *>(out) + at, n, scale); break;
-      case BFS_DTYPE_F16: scale_chunk(static_cast<const _Float16 *>(in) + at, static_cast<float *>(out) + at, n, scale); break;
-      case BFS_DTYPE_BF16 | BFS_DTYPE_BF16 << 4:
-        scale_chunk(static_cast<const __bf16 *>(in) + at, static_cast<__bf16 *>(out) + at, n, scale);
-        break;
-      default:
-        scale_chunk(static_cast<const _Float16 *>(in) + at, static_cast<_Float16 *>(out) + at, n, scale);
-        break;
+    while (t.entry[i].first > c) --i;
+    const Entry e = t.entry[i];
+    if (scale == 1.0f && e.in == e.out) continue;
+    switch (e.type) {
+      case BFS_DTYPE_F32: scale_chunk<float, float>(e, t.chunk, c - e.first, scale); break;
+      case BFS_DTYPE_BF16: scale_chunk<__bf16, float>(e, t.chunk, c - e.first, scale); break;
+      case BFS_DTYPE_F16: scale_chunk<_Float16, float>(e, t.chunk, c - e.first, scale); break;
+      case BFS_DTYPE_BF16 | BFS_DTYPE_BF16 << 4: scale_chunk<__bf16, __bf16>(e, t.chunk, c - e.first, scale); break;
+      default: scale_chunk<_Float16, _Float16>(e, t.chunk, c - e.first, scale); break;
     }
   }
 }
 
-int64_t chunks_of(int64_t n) { return (n + kChunk - 1) / kChunk; }
+int64_t chunks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
 
-// f(list, workgroups, first partial sum) over the tensors that hold something,
-// kTensors at a time; the workgroups go by a list's share of the chunks.
-template <typename F>
-bfs_status each_list(const void *const *in, void *const *out, const int64_t *numel, const int32_t *dtypes,
-                     const int32_t *out_dtypes, int32_t n, int64_t all_chunks, int32_t *n_partial, F f) {
-  TensorList L;
-  int32_t at = 0, partial = 0;
-  while (at < n) {
-    L.n_tensors = 0;
-    int64_t chunks = 0;
-    for (; at < n && L.n_tensors < kTensors; ++at) {
-      if (numel[at] == 0) continue;
-      const int i = L.n_tensors++;
-      L.in[i] = in[at];
-      L.out[i] = out ? out[at] : nullptr;
-      L.n[i] = numel[at];
-      L.first[i] = (int32_t)chunks;
-      L.type[i] = (uint8_t)(dtypes[at] | (out ? out_dtypes[at] << 4 : 0));
-      chunks += chunks_of(numel[at]);
-    }
-    if (L.n_tensors == 0) break;
-    L.n_chunks = (int32_t)chunks;
-    int64_t blocks = (kBlocks * chunks + all_chunks - 1) / all_chunks;
-    blocks = blocks < chunks ? blocks : chunks;
-    bfs_status st = f(L, (int32_t)blocks, partial);
-    if (st != BFS_OK) return st;
-    partial += (int32_t)blocks;
-  }
-  *n_partial = partial;
-  return BFS_OK;
+Table table_of(const bfs_grad_set &set, const void *image) {
+  Table t;
+  t.entry = static_cast<const Entry *>(image);
+  t.start = reinterpret_cast<const int32_t *>(t.entry + set.n_entries);
+  t.chunk = set.chunk;
+  t.n_chunks = set.n_chunks;
+  return t;
 }
 
-bfs_status check_list(const char *what, const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n,
-                      int64_t *all_chunks) {
-  if (n < 0 || (n > 0 && (!grads || !numel || !dtypes))) return fail(BFS_E_INVALID, std::string(what) + ": bad tensor list");
-  *all_chunks = 0;
-  for (int32_t i = 0; i < n; ++i) {
-    if (numel[i] < 0) return fail(BFS_E_INVALID, std::string(what) + ": negative tensor size");
-    if (numel[i] > 0 && !grads[i]) return fail(BFS_E_INVALID, std::string(what) + ": null tensor");
-    if (dtypes[i] < BFS_DTYPE_F32 || dtypes[i] > BFS_DTYPE_F16) return fail(BFS_E_INVALID, std::string(what) + ": unknown dtype");
-    if (numel[i] >> 43 || (*all_chunks += chunks_of(numel[i])) > INT32_MAX)
-      return fail(BFS_E_RESOURCE, std::string(what) + ": more than 2^43 elements");
-  }
-  return BFS_OK;
-}
-
-int64_t workspace_of(int32_t n_tensors) {
-  return ((int64_t)kBlocks + (n_tensors + kTensors - 1) / kTensors + 1) * (int64_t)sizeof(double);
-}
-
-bfs_status check_workspace(const char *what, const void *workspace, int64_t bytes, int32_t n) {
-  if (!workspace || bytes < workspace_of(n))
-    return fail(BFS_E_INVALID, std::string(what) + ": workspace of " + std::to_string(workspace_of(n)) + " bytes needed");
+bfs_status check_call(const char *what, const bfs_grad_set *set, const void *image, const void *workspace, int64_t bytes) {
+  if (!set) return fail(BFS_E_INVALID, std::string(what) + ": null set");
+  if (set->n_entries < 0 || set->n_chunks < set->n_entries || set->n_blocks < 0 || set->n_blocks > kBlocks ||
+      (set->n_chunks > 0 && set->n_blocks < 1) || set->chunk < kMinChunk || set->chunk > kMaxChunk)
+    return fail(BFS_E_INVALID, std::string(what) + ": not a set that bfs_grad_table made");
+  if (set->n_chunks > 0 && (!image || (uintptr_t)image % 16)) return fail(BFS_E_INVALID, std::string(what) + ": bad table address");
+  if (!workspace || bytes < set->workspace_bytes || bytes < set->n_blocks * (int64_t)sizeof(double))
+    return fail(BFS_E_INVALID, std::string(what) + ": workspace of " + std::to_string(set->workspace_bytes) + " bytes needed");
   if ((uintptr_t)workspace % sizeof(double)) return fail(BFS_E_INVALID, std::string(what) + ": workspace not aligned to 8 bytes");
   return BFS_OK;
 }
@@ -219,60 +233,92 @@ bfs_status check_workspace(const char *what, const void *workspace, int64_t byte
 
 extern "C" {
 
-bfs_status bfs_grad_workspace(int32_t n_tensors, int64_t *bytes) {
+bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
+                          const int32_t *out_dtypes, int32_t n_tensors, bfs_grad_set *set, void *image, int64_t image_bytes) {
   return entry([&]() -> bfs_status {
-    if (n_tensors < 0 || !bytes) return fail(BFS_E_INVALID, "grad_workspace: bad argument");
-    *bytes = workspace_of(n_tensors);
+    if (n_tensors < 0 || !set || (n_tensors > 0 && (!grads || !outs || !numel || !dtypes || !out_dtypes)))
+      return fail(BFS_E_INVALID, "grad_table: bad tensor list");
+    int64_t elements = 0;
+    int32_t held = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+      if (numel[i] < 0) return fail(BFS_E_INVALID, "grad_table: negative tensor size");
+      if (numel[i] > 0 && (!grads[i] || !outs[i])) return fail(BFS_E_INVALID, "grad_table: null tensor");
+      if (dtypes[i] < BFS_DTYPE_F32 || dtypes[i] > BFS_DTYPE_F16) return fail(BFS_E_INVALID, "grad_table: unknown dtype");
+      if (out_dtypes[i] != BFS_DTYPE_F32 && out_dtypes[i] != dtypes[i])
+        return fail(BFS_E_INVALID, "grad_table: an output is fp32 or has its gradient's type");
+      if (numel[i] > 0 && grads[i] == outs[i] && out_dtypes[i] != dtypes[i])
+        return fail(BFS_E_INVALID, "grad_table: in place needs the gradient's type");
+      if ((uintptr_t)grads[i] % (dtypes[i] == BFS_DTYPE_F32 ? 4 : 2) || (uintptr_t)outs[i] % (out_dtypes[i] == BFS_DTYPE_F32 ? 4 : 2))
+        return fail(BFS_E_INVALID, "grad_table: a tensor is not aligned to its elements");
+      if (numel[i] > kMaxElements || (elements += numel[i]) > kMaxElements)
+        return fail(BFS_E_RESOURCE, "grad_table: more than 2^43 elements");
+      held += numel[i] > 0;
+    }
+    bfs_grad_set s{};
+    s.chunk = kMaxChunk;
+    while (s.chunk > kMinChunk && elements < s.chunk * kBlocks) s.chunk /= 2;
+    int64_t chunks = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) chunks += chunks_of(numel[i], s.chunk);
+    if (chunks > INT32_MAX) return fail(BFS_E_RESOURCE, "grad_table: more than 2^31 - 1 chunks");
+    s.n_entries = held;
+    s.n_chunks = (int32_t)chunks;
+    s.n_blocks = chunks < kBlocks ? (int32_t)chunks : kBlocks;
+    s.workspace_bytes = (s.n_blocks > 0 ? s.n_blocks : 1) * (int64_t)sizeof(double);
+    s.image_bytes = held * (int64_t)sizeof(Entry) + s.n_blocks * (int64_t)sizeof(int32_t);
+    if (image) {
+      if (image_bytes < s.image_bytes) return fail(BFS_E_INVALID, "grad_table: image of " + std::to_string(s.image_bytes) + " bytes needed");
+      unsigned char *p = static_cast<unsigned char *>(image);
+      int64_t first = 0;
+      int32_t b = 0, k = 0;
+      for (int32_t i = 0; i < n_tensors; ++i) {
+        if (numel[i] == 0) continue;
+        Entry e{};
+        e.in = grads[i];
+        e.out = outs[i];
+        e.n = numel[i];
+        e.first = (int32_t)first;
+        e.chunks = (int32_t)chunks_of(numel[i], s.chunk);
+        e.type = dtypes[i] | out_dtypes[i] << 4;
+        first += e.chunks;
+        // workgroups that begin in this tensor
+        for (; b < s.n_blocks && chunks * b / s.n_blocks < first; ++b)
+          std::memcpy(p + held * sizeof(Entry) + b * sizeof(int32_t), &k, sizeof k);
+        std::memcpy(p + k * sizeof(Entry), &e, sizeof e);
+        ++k;
+      }
+    }
+    *set = s;
     return BFS_OK;
   });
 }
 
-bfs_status bfs_grad_norm(const void *const *grads, const int64_t *numel, const int32_t *dtypes, int32_t n_tensors,
-                         float *norm, void *workspace, int64_t workspace_bytes, struct ihipStream_t *stream) {
+bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *norm, void *workspace,
+                         int64_t workspace_bytes, struct ihipStream_t *stream) {
   return entry([&]() -> bfs_status {
-    int64_t all = 0;
-    bfs_status st = check_list("grad_norm", grads, numel, dtypes, n_tensors, &all);
-    if (st == BFS_OK) st = check_workspace("grad_norm", workspace, workspace_bytes, n_tensors);
+    bfs_status st = check_call("grad_norm", set, dev_image, workspace, workspace_bytes);
     if (st == BFS_OK && !norm) st = fail(BFS_E_INVALID, "grad_norm: null result");
     if (st != BFS_OK) return st;
     double *partial = static_cast<double *>(workspace);
-    int32_t n = 0;
-    st = each_list(grads, nullptr, numel, dtypes, nullptr, n_tensors, all, &n, [&](const TensorList &L, int32_t blocks, int32_t at) {
-      return launch("grad_norm", square_kernel, blocks, kThreads, 0, stream, L, partial + at);
-    });
+    if (set->n_blocks > 0)
+      st = launch("grad_norm", square_kernel, set->n_blocks, kThreads, 0, stream, table_of(*set, dev_image), partial);
     if (st != BFS_OK) return st;
-    return launch("grad_norm", norm_kernel, 1, kThreads, 0, stream, partial, n, norm);
+    return launch("grad_norm", norm_kernel, 1, kThreads, 0, stream, partial, set->n_blocks, norm);
   });
 }
 
-bfs_status bfs_grad_clip(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
-                         const int32_t *out_dtypes, int32_t n_tensors, double max_norm, float *norm, void *workspace,
+bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double max_norm, float *norm, void *workspace,
                          int64_t workspace_bytes, struct ihipStream_t *stream) {
   return entry([&]() -> bfs_status {
-    int64_t all = 0;
-    bfs_status st = check_list("grad_clip", grads, numel, dtypes, n_tensors, &all);
-    if (st == BFS_OK) st = check_workspace("grad_clip", workspace, workspace_bytes, n_tensors);
+    bfs_status st = check_call("grad_clip", set, dev_image, workspace, workspace_bytes);
+    if (st == BFS_OK && !(max_norm >= 0.0)) st = fail(BFS_E_INVALID, "grad_clip: max_norm must not be negative");
     if (st != BFS_OK) return st;
-    if (!(max_norm >= 0.0)) return fail(BFS_E_INVALID, "grad_clip: max_norm must not be negative");
-    if (n_tensors > 0 && (!outs || !out_dtypes)) return fail(BFS_E_INVALID, "grad_clip: bad output list");
-    for (int32_t i = 0; i < n_tensors; ++i) {
-      if (numel[i] > 0 && !outs[i]) return fail(BFS_E_INVALID, "grad_clip: null output");
-      if (out_dtypes[i] != BFS_DTYPE_F32 && out_dtypes[i] != dtypes[i])
-        return fail(BFS_E_INVALID, "grad_clip: an output is fp32 or has its gradient's type");
-    }
     double *partial = static_cast<double *>(workspace);
-    int32_t n = 0, m = 0;
-    st = each_list(grads, outs, numel, dtypes, out_dtypes, n_tensors, all, &n, [&](const TensorList &L, int32_t blocks, int32_t at) {
-      return launch("grad_clip", square_kernel, blocks, kThreads, 0, stream, L, partial + at);
-    });
+    if (set->n_blocks == 0) return norm ? launch("grad_clip", norm_kernel, 1, kThreads, 0, stream, partial, 0, norm) : BFS_OK;
+    const Table t = table_of(*set, dev_image);
+    st = launch("grad_clip", square_kernel, set->n_blocks, kThreads, 0, stream, t, partial);
     if (st != BFS_OK) return st;
-    if (n == 0) return norm ? launch("grad_clip", norm_kernel, 1, kThreads, 0, stream, partial, 0, norm) : BFS_OK;
-    float *first = norm;
-    return each_list(grads, outs, numel, dtypes, out_dtypes, n_tensors, all, &m, [&](const TensorList &L, int32_t blocks, int32_t) {
-      bfs_status s = launch("grad_clip", clip_kernel, blocks, kThreads, 0, stream, L, partial, n, max_norm, first);
-      first = nullptr;
-      return s;
-    });
+    return launch("grad_clip", clip_kernel, set->n_blocks, kThreads, 0, stream,
+                  t, partial, max_norm, norm);
   });
 }
 

@@ -28,8 +28,10 @@ def _refuse(name, what):
     raise BfsError(E_INVALID, f"{name}: {what}")
 
 
-def _current_device():
-    return torch.cuda.current_device()
+# The current device and its current stream's handle, by the bindings that
+# torch.cuda's functions wrap (which take most of a microsecond together).
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: bfs._stream_handle(None))
 
 
 def _dtype(name, t):
@@ -39,39 +41,51 @@ def _dtype(name, t):
     return code
 
 
-def _matrix(name, what, t, device, shape=None, dtype=None, out=False):
-    """Stride between the rows of a [n, width] tensor whose rows have unit
-    stride; an output's rows must not overlap."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != device:
-        _refuse(name, f"{what} must be a tensor on the current device")
-    if dtype is not None and t.dtype is not dtype:
-        _refuse(name, f"{what} must be {dtype}, not {t.dtype}")
+def _first(name, what, t):
+    """The device of a call's first tensor, which must be the current one."""
+    device = t.get_device()
+    if device < 0 or device != _device():
+        _refuse(name, f"{what} must be on the current device")
+    return device
+
+
+def _matrix(name, what, t, device, out=False):
+    """(rows, width, stride between rows) of a tensor of two dimensions whose
+    rows have unit stride; an output's rows must not overlap."""
     size = t.shape
-    if len(size) != 2 or (shape is not None and size != shape):
-        _refuse(name, f"{what} has shape {tuple(size)}, not {'two dimensions' if shape is None else tuple(shape)}")
+    if len(size) != 2 or t.get_device() != device:
+        _refuse(name, f"{what} must have two dimensions and be on the current device, not {tuple(size)}")
     n, width = size
     stride, unit = t.stride()
     if unit != 1 and width > 1:
         _refuse(name, f"{what} must have unit stride in its rows")
     if n <= 1:
-        return width
+        return n, width, width
     if out and stride < width:
         _refuse(name, f"{what} has rows that overlap")
-    return stride
+    return n, width, stride
+
+
+def _matrix_like(name, what, t, device, shape, dtype, out=False):
+    """The stride between the rows of a matrix of a given shape and type."""
+    if t.dtype is not dtype or t.shape != shape:
+        _refuse(name, f"{what} must be {dtype} of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    return _matrix(name, what, t, device, out)[2]
 
 
 def _dense(name, what, t, device, shape, dtype):
     """A contiguous tensor of a given shape and type."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != device:
-        _refuse(name, f"{what} must be a tensor on the current device")
-    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
-        _refuse(name, f"{what} must be contiguous {dtype} of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        _refuse(name, f"{what} must be contiguous {dtype} of shape {tuple(shape)} on the current device, not {t.dtype} "
+                      f"{tuple(t.shape)}")
 
 
-def _stream(name, stream, given):
+def _stream(name, stream, device, given):
     """Handle of the stream; ``given``: whether nothing has to be allocated."""
+    if stream is None:
+        return _raw_stream(device)
     handle = bfs._stream_handle(stream)
-    if stream is not None and not given and handle != bfs._stream_handle(None):
+    if not given and handle != _raw_stream(device):
         _refuse(name, "on another stream than the current one every output and the workspace must be given")
     return handle
 
@@ -89,14 +103,11 @@ def moe_route(logits, k, *, renormalize=True, experts=None, weights=None, stream
     A logit of -inf masks its expert; slots left without one hold -1 and
     weight 0."""
     name = "moe_route"
-    L = bfs._lib or bfs.lib()
-    device = _current_device()
-    stride = _matrix(name, "logits", logits, device)
-    dtype = _dtype(name, logits)
-    t, e = logits.shape
+    device = _first(name, "logits", logits)
+    t, e, stride = _matrix(name, "logits", logits, device)
     if k < 1:
         _refuse(name, f"k = {k}")
-    handle = _stream(name, stream, experts is not None and weights is not None)
+    handle = _stream(name, stream, device, experts is not None and weights is not None)
     shape = (t, k)
     if experts is None:
         experts = logits.new_empty(shape, dtype=torch.int32)
@@ -106,8 +117,11 @@ def moe_route(logits, k, *, renormalize=True, experts=None, weights=None, stream
         weights = logits.new_empty(shape, dtype=torch.float32)
     else:
         _dense(name, "weights", weights, device, shape, torch.float32)
-    _call(L.bfs_moe_route, logits.data_ptr(), dtype, t, e, stride, k, MOE_RENORMALIZE if renormalize else 0,
-          experts.data_ptr(), weights.data_ptr(), handle)
+    status = (bfs._lib or bfs.lib()).bfs_moe_route(
+        logits.data_ptr(), _dtype(name, logits), t, e, stride, k, MOE_RENORMALIZE if renormalize else 0,
+        experts.data_ptr(), weights.data_ptr(), handle)
+    if status:
+        bfs._check(status)
     return experts, weights
 
 
@@ -115,20 +129,22 @@ def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logi
     """The gradient of the logits (of their type) for the gradient of the
     router's weights; ``experts`` and ``renormalize`` as the router had them."""
     name = "moe_route_grad"
-    L = bfs._lib or bfs.lib()
-    device = _current_device()
-    stride = _matrix(name, "logits", logits, device)
-    dtype = _dtype(name, logits)
-    t, e = logits.shape
+    device = _first(name, "logits", logits)
+    t, e, stride = _matrix(name, "logits", logits, device)
     k = experts.shape[-1]
-    _dense(name, "experts", experts, device, (t, k), torch.int32)
-    _dense(name, "grad_weights", grad_weights, device, (t, k), torch.float32)
-    handle = _stream(name, stream, grad_logits is not None)
+    shape = (t, k)
+    _dense(name, "experts", experts, device, shape, torch.int32)
+    _dense(name, "grad_weights", grad_weights, device, shape, torch.float32)
+    handle = _stream(name, stream, device, grad_logits is not None)
     if grad_logits is None:
-        grad_logits = logits.new_empty((t, e))
-    out_stride = _matrix(name, "grad_logits", grad_logits, device, logits.shape, logits.dtype, True)
-    _call(L.bfs_moe_route_grad, logits.data_ptr(), dtype, t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
-          MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride, handle)
+        grad_logits, out_stride = logits.new_empty((t, e)), e
+    else:
+        out_stride = _matrix_like(name, "grad_logits", grad_logits, device, (t, e), logits.dtype, True)
+    status = (bfs._lib or bfs.lib()).bfs_moe_route_grad(
+        logits.data_ptr(), _dtype(name, logits), t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
+        MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride, handle)
+    if status:
+        bfs._check(status)
     return grad_logits
 
 
@@ -149,17 +165,17 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
     without x [T, width].  Entries of perm and rows behind the last row are
     left as they were."""
     name = "moe_dispatch"
-    L = bfs._lib or bfs.lib()
-    device = _current_device()
-    if not isinstance(experts, torch.Tensor) or experts.dim() != 2:
-        _refuse(name, "experts must be a tensor of two dimensions")
+    device = _first(name, "experts", experts)
+    shape = experts.shape
+    if len(shape) != 2:
+        _refuse(name, "experts must have two dimensions")
     if n_experts < 1:
         _refuse(name, f"n_experts = {n_experts}")
-    t, k = shape = experts.shape
+    t, k = shape
     slots = t * k
     _dense(name, "experts", experts, device, shape, torch.int32)
     one_launch = slots <= DISPATCH_ONE_LAUNCH
-    handle = _stream(name, stream, perm is not None and expert_off is not None and pos is not None
+    handle = _stream(name, stream, device, perm is not None and expert_off is not None and pos is not None
                      and (x is None or rows is not None) and (one_launch or workspace is not None))
     if perm is None:
         perm = experts.new_empty(slots)
@@ -173,52 +189,55 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         pos = experts.new_empty(shape)
     else:
         _dense(name, "pos", pos, device, shape, torch.int32)
-    x_ptr = rows_ptr = None
-    dtype = width = x_stride = rows_stride = 0
+    x_ptr = rows_ptr = ws_ptr = None
+    dtype = width = x_stride = rows_stride = ws_bytes = 0
     if x is not None:
-        x_stride = _matrix(name, "x", x, device)
+        n, width, x_stride = _matrix(name, "x", x, device)
         dtype = _dtype(name, x)
-        n, width = x.shape
         if n != t:
             _refuse(name, f"x has {n} rows for {t} tokens")
         if rows is None:
-            rows = x.new_empty((slots, width))
-        rows_stride = _matrix(name, "rows", rows, device, (slots, width), x.dtype, True)
+            rows, rows_stride = x.new_empty((slots, width)), width
+        else:
+            rows_stride = _matrix_like(name, "rows", rows, device, (slots, width), x.dtype, True)
         x_ptr, rows_ptr = x.data_ptr(), rows.data_ptr()
     elif rows is not None:
         _refuse(name, "rows without x")
-    ws_ptr, ws_bytes = None, 0
     if not one_launch:
         if workspace is None:
             workspace = experts.new_empty(moe_dispatch_workspace(t, k, n_experts), dtype=torch.uint8)
-        elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != device or not workspace.is_contiguous():
+        elif workspace.get_device() != device or not workspace.is_contiguous():
             _refuse(name, "workspace must be a contiguous tensor on the current device")
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _call(L.bfs_moe_dispatch, experts.data_ptr(), t, k, n_experts, perm.data_ptr(), expert_off.data_ptr(), pos.data_ptr(),
-          x_ptr, dtype, width, x_stride, rows_ptr, rows_stride, ws_ptr, ws_bytes, handle)
+    status = (bfs._lib or bfs.lib()).bfs_moe_dispatch(
+        experts.data_ptr(), t, k, n_experts, perm.data_ptr(), expert_off.data_ptr(), pos.data_ptr(), x_ptr, dtype, width,
+        x_stride, rows_ptr, rows_stride, ws_ptr, ws_bytes, handle)
+    if status:
+        bfs._check(status)
     return perm, expert_off, pos, rows
 
 
 def _combine(name, rows, pos, weights, out, stream):
-    L = bfs._lib or bfs.lib()
-    device = _current_device()
-    stride = _matrix(name, "rows", rows, device)
-    dtype = _dtype(name, rows)
-    n, width = rows.shape
-    if not isinstance(pos, torch.Tensor) or pos.dim() != 2:
-        _refuse(name, "pos must be a tensor of two dimensions")
-    t, k = shape = pos.shape
+    device = _first(name, "rows", rows)
+    n, width, stride = _matrix(name, "rows", rows, device)
+    shape = pos.shape
+    if len(shape) != 2:
+        _refuse(name, "pos must have two dimensions")
+    t, k = shape
     _dense(name, "pos", pos, device, shape, torch.int32)
     w_ptr = None
     if weights is not None:
         _dense(name, "weights", weights, device, shape, torch.float32)
         w_ptr = weights.data_ptr()
-    handle = _stream(name, stream, out is not None)
+    handle = _stream(name, stream, device, out is not None)
     if out is None:
-        out = rows.new_empty((t, width))
-    out_stride = _matrix(name, "out", out, device, (t, width), rows.dtype, True)
-    _call(L.bfs_moe_combine, rows.data_ptr(), dtype, n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(),
-          out_stride, handle)
+        out, out_stride = rows.new_empty((t, width)), width
+    else:
+        out_stride = _matrix_like(name, "out", out, device, (t, width), rows.dtype, True)
+    status = (bfs._lib or bfs.lib()).bfs_moe_combine(
+        rows.data_ptr(), _dtype(name, rows), n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(), out_stride, handle)
+    if status:
+        bfs._check(status)
     return out
 
 
@@ -241,26 +260,28 @@ def moe_combine_grad(grad_y, rows, pos, weights, *, grad_rows=None, grad_weights
     rows[pos[t, j]]>.  Rows that no slot names are left as they were (zeros in
     a grad_rows that the call allocates)."""
     name = "moe_combine_grad"
-    L = bfs._lib or bfs.lib()
-    device = _current_device()
-    dy_stride = _matrix(name, "grad_y", grad_y, device)
-    dtype = _dtype(name, grad_y)
-    t, width = grad_y.shape
-    rows_stride = _matrix(name, "rows", rows, device, (rows.shape[0], width), grad_y.dtype)
+    device = _first(name, "grad_y", grad_y)
+    t, width, dy_stride = _matrix(name, "grad_y", grad_y, device)
     n = rows.shape[0]
+    rows_stride = _matrix_like(name, "rows", rows, device, (n, width), grad_y.dtype)
     k = pos.shape[-1]
-    _dense(name, "pos", pos, device, (t, k), torch.int32)
-    _dense(name, "weights", weights, device, (t, k), torch.float32)
-    handle = _stream(name, stream, grad_rows is not None and grad_weights is not None)
+    shape = (t, k)
+    _dense(name, "pos", pos, device, shape, torch.int32)
+    _dense(name, "weights", weights, device, shape, torch.float32)
+    handle = _stream(name, stream, device, grad_rows is not None and grad_weights is not None)
     if grad_rows is None:
-        grad_rows = rows.new_zeros((n, width))
-    out_stride = _matrix(name, "grad_rows", grad_rows, device, (n, width), grad_y.dtype, True)
-    if grad_weights is None:
-        grad_weights = weights.new_empty((t, k))
+        grad_rows, out_stride = rows.new_zeros((n, width)), width
     else:
-        _dense(name, "grad_weights", grad_weights, device, (t, k), torch.float32)
-    _call(L.bfs_moe_combine_grad, grad_y.data_ptr(), dtype, t, width, dy_stride, rows.data_ptr(), n, rows_stride,
-          pos.data_ptr(), weights.data_ptr(), k, grad_rows.data_ptr(), out_stride, grad_weights.data_ptr(), handle)
+        out_stride = _matrix_like(name, "grad_rows", grad_rows, device, (n, width), grad_y.dtype, True)
+    if grad_weights is None:
+        grad_weights = weights.new_empty(shape)
+    else:
+        _dense(name, "grad_weights", grad_weights, device, shape, torch.float32)
+    status = (bfs._lib or bfs.lib()).bfs_moe_combine_grad(
+        grad_y.data_ptr(), _dtype(name, grad_y), t, width, dy_stride, rows.data_ptr(), n, rows_stride, pos.data_ptr(),
+        weights.data_ptr(), k, grad_rows.data_ptr(), out_stride, grad_weights.data_ptr(), handle)
+    if status:
+        bfs._check(status)
     return grad_rows, grad_weights
 
 
@@ -270,8 +291,10 @@ class GradSet:
     ``grads``: contiguous float32, bfloat16 or float16 tensors.  ``out``: None
     (they are clipped in place), a flat tensor that takes them one after the
     other (float32, or the type of all of them: the gradient buffer of an
-    AdamW plan), or a tensor for each.  The set keeps the tensors' memory: a
-    gradient that is allocated anew needs a new set."""
+    AdamW plan), or a tensor for each.  Like a plan its program, the set keeps
+    a table of the tensors on the device, and their memory: a gradient that is
+    allocated anew needs a new set.  Making one copies the table (it waits for
+    the copy and cannot be captured); the calls can be."""
 
     def __init__(self, grads, out=None):
         name = "GradSet"
@@ -303,37 +326,41 @@ class GradSet:
         # aliases: the memory stays even where a tensor's data is exchanged
         self._keep = [t.detach() for t in [*grads, *outs]]
         self._device = devices.pop() if devices else None
-        self._home = grads[0].device if grads else None
-        n = self._n = len(grads)
-        self._grads = struct.pack("%dP" % n, *[g.data_ptr() for g in grads])
-        self._outs = struct.pack("%dP" % n, *[o.data_ptr() for o in outs])
-        self._sizes = struct.pack("%dq" % n, *sizes)
-        self._types = struct.pack("%di" % n, *types)
-        self._out_types = struct.pack("%di" % n, *[DTYPES[o.dtype] for o in outs])
-        bytes_ = C.c_int64()
-        _call(bfs.lib().bfs_grad_workspace, n, C.byref(bytes_))
-        self.workspace_bytes = bytes_.value
+        n = len(grads)
+        arrays = (struct.pack("%dP" % n, *[g.data_ptr() for g in grads]), struct.pack("%dP" % n, *[o.data_ptr() for o in outs]),
+                  struct.pack("%dq" % n, *sizes), struct.pack("%di" % n, *types),
+                  struct.pack("%di" % n, *[DTYPES[o.dtype] for o in outs]), n)
+        table = bfs.lib().bfs_grad_table
+        self._set = bfs.GradSetStruct()
+        _call(table, *arrays, C.byref(self._set), None, 0)
+        size = self._set.image_bytes
+        self._table = None
+        if size:
+            image = bytearray(size)
+            _call(table, *arrays, C.byref(self._set), (C.c_char * size).from_buffer(image), size)
+            self._table = torch.frombuffer(image, dtype=torch.uint8).to(grads[0].device)     # waits for the copy
+        self._args = C.byref(self._set), None if self._table is None else self._table.data_ptr()
+        self.workspace_bytes = self._set.workspace_bytes
 
     def _buffers(self, name, norm, workspace, stream):
-        device = _current_device()
-        if self._device is not None and device != self._device:
+        device = _device()
+        if device != self._device and self._device is not None:
             _refuse(name, "the gradients are not on the current device")
-        handle = _stream(name, stream, norm is not None and workspace is not None)
+        handle = _stream(name, stream, device, norm is not None and workspace is not None)
         if norm is None:
             norm = torch.empty((), dtype=torch.float32, device="cuda")
         else:
             _dense(name, "norm", norm, device, (), torch.float32)
         if workspace is None:
-            workspace = norm.new_empty(self.workspace_bytes, dtype=torch.uint8)
-        elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != device or not workspace.is_contiguous():
+            return norm, norm.new_empty(self.workspace_bytes, dtype=torch.uint8), self.workspace_bytes, handle
+        if workspace.get_device() != device or not workspace.is_contiguous():
             _refuse(name, "workspace must be a contiguous tensor on the current device")
         return norm, workspace, workspace.numel() * workspace.element_size(), handle
 
     def norm(self, norm=None, workspace=None, stream=None):
         """The global norm, a float32 scalar on the device."""
         norm, workspace, size, handle = self._buffers("grad_norm", norm, workspace, stream)
-        _call(bfs.lib().bfs_grad_norm, self._grads, self._sizes, self._types, self._n, norm.data_ptr(),
-              workspace.data_ptr(), size, handle)
+        _call(bfs._lib.bfs_grad_norm, *self._args, norm.data_ptr(), workspace.data_ptr(), size, handle)
         return norm
 
     def clip(self, max_norm, norm=None, workspace=None, stream=None):
@@ -341,16 +368,15 @@ class GradSet:
         returns the norm before clipping.  A norm that is not finite scales by
         1."""
         norm, workspace, size, handle = self._buffers("grad_clip", norm, workspace, stream)
-        _call(bfs.lib().bfs_grad_clip, self._grads, self._outs, self._sizes, self._types, self._out_types, self._n, max_norm,
-              norm.data_ptr(), workspace.data_ptr(), size, handle)
+        _call(bfs._lib.bfs_grad_clip, *self._args, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle)
         return norm
 
 
 def grad_norm(grads, **kw):
-    """GradSet(grads).norm(), for gradients that are used once."""
+    """GradSet(grads).norm(), for gradients that are used once (not captured)."""
     return GradSet(grads).norm(**kw)
 
 
 def grad_clip(grads, max_norm, out=None, **kw):
-    """GradSet(grads, out).clip(max_norm), for gradients that are used once."""
+    """GradSet(grads, out).clip(max_norm), for gradients that are used once (not captured)."""
     return GradSet(grads, out).clip(max_norm, **kw)

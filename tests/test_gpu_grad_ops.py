@@ -136,7 +136,7 @@ def test_refusals():
                  lambda: GradSet([g], out=g.half()), lambda: GradSet([g], out=[]), lambda: GradSet([g], out=[g[:4]]),
                  lambda: GradSet([g.half()], out=[g.bfloat16()]), lambda: GradSet([g]).clip(-1.0),
                  lambda: GradSet([g]).clip(float("nan")), lambda: GradSet([g]).norm(norm=torch.empty(1, device="cuda")),
-                 lambda: GradSet([g]).norm(workspace=torch.empty(8, device="cuda")),
+                 lambda: GradSet([g]).norm(workspace=torch.empty(1, dtype=torch.uint8, device="cuda")),
                  lambda: GradSet([g]).norm(stream=torch.cuda.Stream())):
         with pytest.raises(BfsError) as e:
             call()

@@ -142,6 +142,8 @@ class _Step:
         self.k, self.e = k, e
         self.logits, self.x, self.dy = _normal(seed, (t, e), dtype), _normal(seed + 1, (t, h), dtype), _normal(seed + 2, (t, h), dtype)
         self.grads = [_normal(seed + 3, (n,), torch.float32) for n in (4000, 17, 30000)]
+        self.flat = torch.empty(34017, device="cuda")
+        self.set = GradSet(self.grads, out=self.flat)
 
     def refill(self, seed):
         for i, a in enumerate((self.logits, self.x, self.dy, *self.grads)):
@@ -157,9 +159,8 @@ class _Step:
         drows, dw = bfsp.moe_combine_grad(self.dy, rows, pos, w)
         dx = bfsp.moe_dispatch_grad(drows, pos)
         dz = bfsp.moe_route_grad(self.logits, experts, dw)
-        flat = torch.empty(34017, device="cuda")
-        norm = GradSet(self.grads, out=flat).clip(1.0)
-        return [experts, w, perm, off, pos, rows, y, drows, dw, dx, dz, flat, norm]
+        norm = self.set.clip(1.0)
+        return [experts, w, perm, off, pos, rows, y, drows, dw, dx, dz, self.flat.clone(), norm]
 
 
 @pytest.mark.parametrize("t,e,k,h,dtype", [(9, 16, 2, 64, torch.bfloat16), (3000, 64, 4, 136, torch.float16),

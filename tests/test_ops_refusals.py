@@ -45,14 +45,24 @@ def _list(values, kind):
     return (kind * max(1, len(values)))(*values)
 
 
-def _norm(grads=(A,), numel=(4,), dtypes=(F32,), n=None, norm=A, ws=A, ws_bytes=1 << 20):
-    return _status("bfs_grad_norm", _list(grads, C.c_void_p), _list(numel, C.c_int64), _list(dtypes, C.c_int32),
-                   len(grads) if n is None else n, norm, ws, ws_bytes, None)
+def _table(grads=(A,), outs=(A,), numel=(4,), dtypes=(F32,), out_dtypes=(F32,), n=None, image=False, image_bytes=1 << 20,
+           made=True):
+    made = bfs.GradSetStruct() if made else None
+    buf = C.create_string_buffer(1 << 20) if image else None
+    st = _status("bfs_grad_table", _list(grads, C.c_void_p), _list(outs, C.c_void_p), _list(numel, C.c_int64),
+                 _list(dtypes, C.c_int32), _list(out_dtypes, C.c_int32), len(grads) if n is None else n,
+                 C.byref(made) if made is not None else None, buf, image_bytes)
+    return st if st != bfs.OK else (made, buf)
 
 
-def _clip(grads=(A,), outs=(A,), numel=(4,), dtypes=(F32,), out_dtypes=(F32,), max_norm=1.0, ws=A, ws_bytes=1 << 20):
-    return _status("bfs_grad_clip", _list(grads, C.c_void_p), _list(outs, C.c_void_p), _list(numel, C.c_int64),
-                   _list(dtypes, C.c_int32), _list(out_dtypes, C.c_int32), len(grads), max_norm, A, ws, ws_bytes, None)
+def _grad_call(change=None, image=A, ws=A, ws_bytes=1 << 20, set_=True, **kw):
+    made, _ = _table()
+    if change:
+        setattr(made, *change)
+    made = C.byref(made) if set_ else None
+    if "max_norm" in kw:
+        return _status("bfs_grad_clip", made, image, kw["max_norm"], A, ws, ws_bytes, None)
+    return _status("bfs_grad_norm", made, image, kw.get("norm", A), ws, ws_bytes, None)
 
 
 INVALID = [
@@ -73,11 +83,15 @@ INVALID = [
     (_combine_grad, dict(out_stride=15)), (_combine_grad, dict(dy_stride=-1)), (_combine_grad, dict(stride=-1)),
     (_combine_grad, dict(w=None)), (_combine_grad, dict(dw=None)), (_combine_grad, dict(dy=None)),
     (_combine_grad, dict(rows=None)), (_combine_grad, dict(out=None)), (_combine_grad, dict(dtype=5)),
-    (_norm, dict(n=-1)), (_norm, dict(numel=(-4,))), (_norm, dict(grads=(None,))), (_norm, dict(dtypes=(3,))),
-    (_norm, dict(norm=None)), (_norm, dict(ws=None)), (_norm, dict(ws_bytes=64)), (_norm, dict(ws=A + 4)),
-    (_clip, dict(max_norm=-1.0)), (_clip, dict(max_norm=float("nan"))), (_clip, dict(outs=(None,))),
-    (_clip, dict(out_dtypes=(BF16,))), (_clip, dict(dtypes=(BF16,), out_dtypes=(F16,))), (_clip, dict(out_dtypes=(9,))),
-    (_clip, dict(ws=None)), (_clip, dict(ws_bytes=0)),
+    (_table, dict(n=-1)), (_table, dict(numel=(-4,))), (_table, dict(grads=(None,))), (_table, dict(outs=(None,))),
+    (_table, dict(dtypes=(3,))), (_table, dict(out_dtypes=(BF16,))), (_table, dict(dtypes=(BF16,), out_dtypes=(F16,))),
+    (_table, dict(out_dtypes=(9,))), (_table, dict(dtypes=(BF16,))), (_table, dict(grads=(A + 2,))),
+    (_table, dict(outs=(A + 1,), dtypes=(BF16,), out_dtypes=(BF16,))), (_table, dict(image=True, image_bytes=8)),
+    (_table, dict(made=False)), (_grad_call, dict(set_=False)), (_grad_call, dict(image=None)), (_grad_call, dict(image=A + 8)),
+    (_grad_call, dict(norm=None)), (_grad_call, dict(ws=None)), (_grad_call, dict(ws_bytes=4)), (_grad_call, dict(ws=A + 4)),
+    (_grad_call, dict(max_norm=-1.0)), (_grad_call, dict(max_norm=float("nan"))), (_grad_call, dict(max_norm=1.0, ws=None)),
+    (_grad_call, dict(change=("n_blocks", 0))), (_grad_call, dict(change=("n_blocks", 1 << 20))),
+    (_grad_call, dict(change=("chunk", 0))), (_grad_call, dict(change=("n_entries", -1))),
 ]
 
 
@@ -90,7 +104,8 @@ def test_invalid_arguments(call, kw):
 RESOURCE = [(_route, dict(e=1025, stride=1025)), (_route, dict(e=64, stride=64, k=17)), (_route, dict(t=1 << 31)),
             (_dispatch, dict(e=1025)), (_dispatch, dict(k=65)), (_dispatch, dict(t=1 << 30)), (_combine, dict(k=65)),
             (_combine, dict(t=1 << 30)), (_combine, dict(n=1 << 31)), (_combine_grad, dict(t=1 << 30)),
-            (_norm, dict(numel=(1 << 44,))), (_norm, dict(grads=(A, A), numel=(1 << 42, 1 << 43), dtypes=(F32, F32)))]
+            (_table, dict(numel=(1 << 44,))),
+            (_table, dict(grads=(A, A), outs=(A, A), numel=(1 << 42, 1 << 43), dtypes=(F32, F32), out_dtypes=(F32, F32)))]
 
 
 @pytest.mark.parametrize("call,kw", RESOURCE, ids=lambda v: getattr(v, "__name__", str(v)))
@@ -110,18 +125,43 @@ def test_nothing_to_do():
 def test_workspaces():
     torch = pytest.importorskip("torch")
     from paper_2608_13757_amd import GradSet, moe_dispatch_workspace
-    assert moe_dispatch_workspace(1, 1, 64) == 0
+    from paper_2608_13757_amd.ops import DISPATCH_ONE_LAUNCH
+    assert moe_dispatch_workspace(1, 1, 64) == 0 and moe_dispatch_workspace(DISPATCH_ONE_LAUNCH, 1, 64) == 0
+    assert moe_dispatch_workspace(DISPATCH_ONE_LAUNCH + 1, 1, 64) > 0
     assert moe_dispatch_workspace(32768, 2, 64) > 0
     for bad in ((-1, 1, 4), (4, 0, 4), (4, 1, 0)):
         with pytest.raises(BfsError) as e:
             moe_dispatch_workspace(*bad)
         assert e.value.status == bfs.E_INVALID
-    n = C.c_int64()
-    assert _status("bfs_grad_workspace", -1, C.byref(n)) == bfs.E_INVALID
-    assert _status("bfs_grad_workspace", 3, None) == bfs.E_INVALID
-    assert _status("bfs_grad_workspace", 0, C.byref(n)) == bfs.OK and n.value > 0
     with pytest.raises(BfsError):
         GradSet([torch.zeros(3)])                     # not on a device
+
+
+def _entries(made, buf):
+    """(in, out, n, first, chunks, type) of each tensor, and each workgroup's first one."""
+    import struct
+    raw = buf.raw[:made.image_bytes]
+    rows = [struct.unpack_from("<QQqiiii", raw, 40 * i)[:6] for i in range(made.n_entries)]
+    return rows, struct.unpack_from("<%di" % made.n_blocks, raw, 40 * made.n_entries)
+
+
+@pytest.mark.parametrize("sizes", [[1], [5, 0, 100000, 3, 0, 16384], [1] * 2000, [7] + [1 << 20] * 30, [1 << 33, 9], []])
+def test_grad_table(sizes):
+    """Every tensor's chunks cover it, in order; a workgroup's first chunk
+    lies in the tensor that the table names."""
+    n = len(sizes)
+    got = _table([A] * n, [A] * n, sizes, [BF16] * n, [BF16] * n, image=True, image_bytes=1 << 20)
+    made, buf = got
+    rows, start = _entries(made, buf)
+    assert [r[2] for r in rows] == [s for s in sizes if s] and all(r[0] == r[1] == A and r[5] == BF16 * 17 for r in rows)
+    at = 0
+    for _, _, size, first, chunks, _ in rows:
+        assert first == at and (chunks - 1) * made.chunk < size <= chunks * made.chunk
+        at += chunks
+    assert at == made.n_chunks and made.n_blocks == min(at, 1024) == len(start)
+    for b, i in enumerate(start):
+        c = made.n_chunks * b // made.n_blocks
+        assert rows[i][3] <= c < rows[i][3] + rows[i][4]
 
 
 def test_package_imports_without_the_operators():
