@@ -22,7 +22,6 @@
 // passes, a large copy's rate; 2^20 fp32 in 24: 9 us, two short launches.
 #include <cmath>
 #include <cstring>
-#include <tuple>
 
 #include "op_common.h"
 

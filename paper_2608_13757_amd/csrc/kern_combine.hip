@@ -12,11 +12,15 @@
 // gradient's rows are written once each, without atomics.  Positions outside
 // 0 .. n_rows - 1 count as slots without a row.
 //
-// Everything is one pass over the rows, bound by memory: a wave takes a token
-// (or, for few tokens, a span of its row), 16 bytes per lane and access, with
-// the loads of up to four slots in flight together.
-#include <tuple>
-
+// Everything is one pass over the rows, bound by memory: 16 bytes per lane and
+// access, up to 16 loads of a lane in flight (four slots, four steps of the
+// row; the gradient two, with dy's).  In the combination a wave takes a token's
+// row or a part of it (op_common.h: spans_of); in the gradient, whose dot
+// products join the whole row, a workgroup takes a token where its four waves
+// have a step each, else a wave does (32768 tokens, two rows of 4096 bf16: 246
+// us, with a wave for each token 256; one row of 1024: 76 and 35 us).
+// 16384 tokens of eight rows of 2048 bf16, 605 MB: 100 us (6.0 TB/s; a large
+// copy runs at 5.3), its gradient, 1.14 GB, 203 us (5.6).
 #include "op_common.h"
 
 using namespace bfsop;
@@ -51,69 +55,168 @@ __device__ __forceinline__ float readlane(float x, int j) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), j));
 }
 
-template <typename T>
+// f(N, slots) for the slots whose bits are set, four at once, then two, one;
+// in their order.
+template <typename F>
+__device__ __forceinline__ void each_slots(uint64_t set, F f) {
+  auto take = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    int j[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      j[i] = __builtin_ctzll(set);
+      set &= set - 1;
+    }
+    f(n, j);
+  };
+  while (__builtin_popcountll(set) >= 4) take(Int<4>{});
+  if (__builtin_popcountll(set) >= 2) take(Int<2>{});
+  if (set) take(Int<1>{});
+}
+
+// A wave takes a token, or one of `spans` interleaved parts of its row.
+template <typename T, int kSteps, bool kStream>
 __global__ void __launch_bounds__(kThreads) combine_kernel(CombineParams P) {
   constexpr int E = Chunk<T>::kElems;
+  typedef typename Chunk<T>::vec vec;
   const int64_t u = (int64_t)blockIdx.x * kBlockWaves + wave_index();
   const int64_t t = u / P.spans;
   if (t >= P.n_tokens) return;
-  const int64_t chunks = (P.width + E - 1) / E, step = (int64_t)P.spans * kWave;
+  const int lane = lane_index();
+  const int64_t span = u - t * P.spans, chunks = P.width / E, step = (int64_t)P.spans * kWave;
   const T *rows = static_cast<const T *>(P.rows);
   T *y = static_cast<T *>(P.out) + t * P.out_stride;
   int slot;
   float weight;
-  load_slot(P, t, lane_index(), slot, weight);
-  for (int64_t c = (u - t * P.spans) * kWave + lane_index(); c < chunks; c += step) {
-    float acc[E];
+  load_slot(P, t, lane, slot, weight);
+  const uint64_t set = __ballot(slot >= 0);
+  each_chunk<kSteps>(span * kWave + lane, chunks, step, [&](auto us, int64_t c) {
+    constexpr int U = decltype(us)::value;
+    float acc[U][E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) acc[i] = 0.0f;
-    for (int j = 0; j < P.k; ++j) {
-      const int64_t p = __builtin_amdgcn_readlane(slot, j);
-      if (p < 0) continue;
-      const float w = readlane(weight, j);
-      const auto v = load_chunk<T>(rows + p * P.rows_stride, c, P.width);
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < E; ++i) acc[i] += w * (float)v[i];
+      for (int i = 0; i < E; ++i) acc[u][i] = 0.0f;
+    each_slots(set, [&](auto ns, const int *j) {
+      constexpr int N = decltype(ns)::value;
+      vec v[N][U];
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const T *row = rows + __builtin_amdgcn_readlane(slot, j[n]) * P.rows_stride;
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[n][u] = load<kStream>(row + (c + u * step) * E);
+      }
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float w = readlane(weight, j[n]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int i = 0; i < E; ++i) acc[u][i] += w * (float)v[n][u][i];
+      }
+    });
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      vec o;
+#pragma unroll
+      for (int i = 0; i < E; ++i) o[i] = (T)acc[u][i];
+      store<kStream>(y + (c + u * step) * E, o);
     }
-    typename Chunk<T>::vec o;
+  });
+  const int64_t i = chunks * E + lane;             // the elements behind the last whole chunk
+  if (span == 0 && i < P.width) {
+    float acc = 0.0f;
+    each_slots(set, [&](auto ns, const int *j) {
+      constexpr int N = decltype(ns)::value;
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = (T)acc[i];
-    store_chunk<T>(y, c, P.width, o);
+      for (int n = 0; n < N; ++n)
+        acc += readlane(weight, j[n]) * (float)rows[__builtin_amdgcn_readlane(slot, j[n]) * P.rows_stride + i];
+    });
+    y[i] = (T)acc;
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) combine_grad_kernel(CombineParams P) {
-  constexpr int E = Chunk<T>::kElems;
-  const int64_t t = (int64_t)blockIdx.x * kBlockWaves + wave_index();
-  if (t >= P.n_tokens) return;
-  const int lane = lane_index();
-  const int64_t chunks = (P.width + E - 1) / E;
-  const T *rows = static_cast<const T *>(P.rows), *dy = static_cast<const T *>(P.dy) + t * P.dy_stride;
+// <dy, rows[p_n]> over this lane's part of the rows, and rows of w_n * dy; for
+// N slots.
+template <typename T, int N, bool kStream>
+__device__ __forceinline__ void grad_slots(const CombineParams &P, const T *dy, const int64_t *p, const float *w, int64_t at,
+                                           int64_t step, float (&dot)[N]) {
+  constexpr int E = Chunk<T>::kElems, kMost = N == 4 ? 2 : 4;
+  typedef typename Chunk<T>::vec vec;
+  const int64_t chunks = P.width / E;
+  const T *rows = static_cast<const T *>(P.rows);
   T *out = static_cast<T *>(P.out);
-  int slot;
-  float weight;
-  load_slot(P, t, lane, slot, weight);
-  for (int j = 0; j < P.k; ++j) {
-    const int64_t p = __builtin_amdgcn_readlane(slot, j);
-    float dot = 0.0f;
-    if (p >= 0) {
-      const float w = readlane(weight, j);
-      for (int64_t c = lane; c < chunks; c += kWave) {
-        const auto g = load_chunk<T>(dy, c, P.width);
-        const auto v = load_chunk<T>(rows + p * P.rows_stride, c, P.width);
-        typename Chunk<T>::vec o;
+#pragma unroll
+  for (int n = 0; n < N; ++n) dot[n] = 0.0f;
+  each_chunk<kMost>(at, chunks, step, [&](auto us, int64_t c) {
+    constexpr int U = decltype(us)::value;
+    vec g[U], v[N][U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) g[u] = *reinterpret_cast<const vec *>(dy + (c + u * step) * E);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        v[n][u] = load<kStream>(rows + p[n] * P.rows_stride + (c + u * step) * E);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        vec o;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-          dot += (float)g[i] * (float)v[i];
-          o[i] = (T)(w * (float)g[i]);
+          dot[n] += (float)g[u][i] * (float)v[n][u][i];
+          o[i] = (T)(w[n] * (float)g[u][i]);
         }
-        store_chunk<T>(out + p * P.out_stride, c, P.width, o);
+        store<kStream>(out + p[n] * P.out_stride + (c + u * step) * E, o);
       }
+  });
+  const int64_t i = chunks * E + at;
+  if (at < E && i < P.width) {
+    const float g = (float)dy[i];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      dot[n] += g * (float)rows[p[n] * P.rows_stride + i];
+      out[p[n] * P.out_stride + i] = (T)(w[n] * g);
     }
-    dot = group_sum<64>(dot);
-    if (lane == 0) P.grad_weights[t * P.k + j] = dot;
   }
+}
+
+// W waves take a token.
+template <typename T, int W, bool kStream>
+__global__ void __launch_bounds__(kThreads) combine_grad_kernel(CombineParams P) {
+  __shared__ float part[W > 1 ? W : 1][kMaxK];
+  const int64_t t = ((int64_t)blockIdx.x * kBlockWaves + wave_index()) / W;
+  if (t >= P.n_tokens) return;
+  const int lane = lane_index(), wave = wave_index() % W;
+  int slot;
+  float weight, grad = 0.0f;                       // lane j: of slot j
+  load_slot(P, t, lane, slot, weight);
+  each_slots(__ballot(slot >= 0), [&](auto ns, const int *j) {
+    constexpr int N = decltype(ns)::value;
+    int64_t p[N];
+    float w[N], dot[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      p[n] = __builtin_amdgcn_readlane(slot, j[n]);
+      w[n] = readlane(weight, j[n]);
+    }
+    grad_slots<T, N, kStream>(P, static_cast<const T *>(P.dy) + t * P.dy_stride, p, w, wave * kWave + lane, W * kWave, dot);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float d = group_sum<64>(dot[n]);
+      if (lane == j[n]) grad = d;
+    }
+  });
+  if (W > 1) {                                     // the workgroup's only token
+    part[wave][lane] = grad;
+    __syncthreads();
+    if (wave != 0) return;
+    grad = 0.0f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) grad += part[i][lane];
+  }
+  if (lane < P.k) P.grad_weights[t * P.k + lane] = grad;
 }
 
 bfs_status check_rows(const char *what, int64_t n_rows, int64_t width, int64_t n_tokens, int32_t k) {
@@ -152,9 +255,13 @@ bfs_status bfs_moe_combine(const void *rows, int32_t dtype, int64_t n_rows, int6
       P.out_stride = y_stride;
       P.k = k;
       const int64_t chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
-      const int64_t most = (chunks + kWave - 1) / kWave, wanted = (4096 + n_tokens - 1) / n_tokens;
-      P.spans = (int32_t)(most < wanted ? most : wanted);
-      return launch("moe_combine", combine_kernel<T>, (n_tokens * P.spans + kBlockWaves - 1) / kBlockWaves, kThreads, 0,
+      const int64_t most = (chunks + kWave - 1) / kWave;
+      P.spans = (int32_t)spans_of(most, n_tokens);
+      // chunks of a lane at once: four where a wave's part of the row has them
+      auto kernel = most >= 4 * P.spans ? combine_kernel<T, 4, false> : combine_kernel<T, 2, false>;
+      if ((k + 1) * n_tokens * width * (int64_t)sizeof(T) >= kStreamFrom)
+        kernel = most >= 4 * P.spans ? combine_kernel<T, 4, true> : combine_kernel<T, 2, true>;
+      return launch("moe_combine", kernel, (n_tokens * P.spans + kBlockWaves - 1) / kBlockWaves, kThreads, 0,
                     stream, P);
     });
   });
@@ -188,8 +295,13 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
       P.dy_stride = grad_y_stride;
       P.out_stride = grad_rows_stride;
       P.k = k;
-      return launch("moe_combine_grad", combine_grad_kernel<T>, (n_tokens + kBlockWaves - 1) / kBlockWaves, kThreads, 0,
-                    stream, P);
+      const bool stream_rows = (2 * k + 1) * n_tokens * width * (int64_t)sizeof(T) >= kStreamFrom;
+      if (width / Chunk<T>::kElems >= kThreads)
+        return launch("moe_combine_grad",
+                      stream_rows ? combine_grad_kernel<T, kBlockWaves, true> : combine_grad_kernel<T, kBlockWaves, false>,
+                      n_tokens, kThreads, 0, stream, P);
+      return launch("moe_combine_grad", stream_rows ? combine_grad_kernel<T, 1, true> : combine_grad_kernel<T, 1, false>,
+                    (n_tokens + kBlockWaves - 1) / kBlockWaves, kThreads, 0, stream, P);
     });
   });
 }

@@ -12,12 +12,18 @@
 // adds the counts of the earlier batches, waves and groups of slots, so that
 // rows come in the same order in every run.  LDS atomics only count.
 //
-// Up to kSmallSlots slots one launch does all: every workgroup ranks all the
-// slots by itself and copies its share of the rows.  Beyond, three: counts of
-// each group of slots; ranks, every group summing the counts of the groups
-// before it; the copy.
-#include <tuple>
-
+// The slots go in groups of up to 1024, a workgroup ranks a whole group.  Before
+// several groups one launch counts each group's slots by expert, and the
+// ranking workgroups sum the groups before theirs, or, where that table is long,
+// read sums that one more launch makes.  The rows are copied by the ranking
+// workgroups where 1024 of them give each wave one part of a row: several then
+// rank the same group, each for itself, and one launch is saved (2048 tokens of
+// 4096 bf16 to 8 experts each: 33.4 us, with the copy in a launch of its own
+// 35.6; 128 tokens to two: 5 us in a single launch).  Beyond, the copy is a
+// launch of its own, whose waves end with their stores under way.
+//
+// Bound by memory: 32768 tokens of 4096 bf16 to two experts of 64 each, 806 MB,
+// in 156 us (5.2 TB/s, a large copy's rate), some 8 us of them the ranking.
 #include "op_common.h"
 
 using namespace bfsop;
@@ -25,28 +31,30 @@ using namespace bfsop;
 namespace {
 
 constexpr int kMaxExperts = 1024, kMaxK = 64;
-constexpr int kSmallWaves = 4, kSmallSlots = 1024;
-constexpr int kGroupWaves = 16, kGroupSlots = 4096;
+constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kBatches = 4;                            // batches of 64 slots per wave
-static_assert(kSmallSlots == kSmallWaves * kBatches * kWave && kGroupSlots == kGroupWaves * kBatches * kWave, "");
+constexpr int kGroupSlots = kWaves * kBatches * kWave;
+constexpr int kBlocks = 1024;                          // workgroups that rank and copy, at most
+constexpr int64_t kSumEntries = 8192;                  // counts that every workgroup sums by itself
 
 struct DispatchParams {
   const int32_t *experts;
   const void *x;
   int32_t *perm, *off, *pos;
   void *rows;
-  uint32_t *counts;              // [groups][n_experts]
-  int64_t n_slots, x_stride, rows_stride, width;
-  int32_t k, n_experts, n_groups, bits;
+  uint32_t *counts;              // [n_groups][n_experts]; with sums: of the groups before, and [n_groups]: of all
+  int64_t n_slots, x_stride, rows_stride, width, spans;
+  int32_t k, n_experts, n_groups, group, parts, bits;   // group: slots of one, whole tokens
 };
 
-// The ids of this lane's slots: wave w holds batches w * kBatches ... of the
-// group that starts at `first`; -1 without an expert or past the end.
-__device__ __forceinline__ void load_ids(const DispatchParams &P, int64_t first, int wave, int lane, int (&id)[kBatches]) {
+// The ids of this lane's slots of group g: wave w holds batches
+// w * kBatches ...; -1 without an expert or past the end.
+__device__ __forceinline__ void load_ids(const DispatchParams &P, int g, int wave, int lane, int (&id)[kBatches]) {
 #pragma unroll
   for (int b = 0; b < kBatches; ++b) {
-    const int64_t s = first + (wave * kBatches + b) * kWave + lane;
-    const int e = s < P.n_slots ? P.experts[s] : -1;
+    const int i = (wave * kBatches + b) * kWave + lane;
+    const int64_t s = (int64_t)g * P.group + i;
+    const int e = i < P.group && s < P.n_slots ? P.experts[s] : -1;
     id[b] = (uint32_t)e < (uint32_t)P.n_experts ? e : -1;
   }
 }
@@ -54,17 +62,16 @@ __device__ __forceinline__ void load_ids(const DispatchParams &P, int64_t first,
 // Counts of each wave's slots by expert, then for each wave the slots of the
 // waves before it; total[e] the group's.  hist: [kWaves][n_experts], zeroed
 // here.
-template <int kWaves>
 __device__ __forceinline__ void count_waves(const DispatchParams &P, const int (&id)[kBatches], int wave, uint32_t *hist,
                                             uint32_t *total) {
   const int E = P.n_experts;
-  for (int i = (int)threadIdx.x; i < kWaves * E; i += kWaves * kWave) hist[i] = 0;
+  for (int i = (int)threadIdx.x; i < kWaves * E; i += kThreads) hist[i] = 0;
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < kBatches; ++b)
     if (id[b] >= 0) atomicAdd(&hist[wave * E + id[b]], 1u);
   __syncthreads();
-  for (int e = (int)threadIdx.x; e < E; e += kWaves * kWave) {
+  for (int e = (int)threadIdx.x; e < E; e += kThreads) {
     uint32_t run = 0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
@@ -102,7 +109,6 @@ __device__ __forceinline__ void expert_starts(int n_experts, const uint32_t *tot
 // first row of the group's slots of e, hist the wave's slots before it.  A
 // wave's LDS accesses complete in order, so a batch sees the counts that the
 // batch before it left.
-template <int kWaves>
 __device__ __forceinline__ void rank_slots(const DispatchParams &P, const int (&id)[kBatches], int wave, int lane,
                                            uint32_t *hist, const uint32_t *base, int (&row)[kBatches]) {
   const int E = P.n_experts;
@@ -129,115 +135,155 @@ __device__ __forceinline__ void rank_slots(const DispatchParams &P, const int (&
   }
 }
 
-// pos and perm of this lane's slots.
-__device__ __forceinline__ void store_ranks(const DispatchParams &P, int64_t first, int wave, int lane, const int (&row)[kBatches]) {
-#pragma unroll
-  for (int b = 0; b < kBatches; ++b) {
-    const int64_t s = first + (wave * kBatches + b) * kWave + lane;
-    if (s < P.n_slots) {
-      P.pos[s] = row[b];
-      if (row[b] >= 0) P.perm[row[b]] = (int32_t)(s / P.k);
+// Slots by expert of the groups before g, and of all groups.  With fewer
+// experts than threads several threads share an expert's groups.
+__device__ __forceinline__ void sum_groups(const DispatchParams &P, int g, uint32_t *before, uint32_t *total) {
+  const int E = P.n_experts;
+  if (P.n_groups * (int64_t)E > kSumEntries) {
+    for (int e = (int)threadIdx.x; e < E; e += kThreads) {
+      before[e] = P.counts[(int64_t)g * E + e];
+      total[e] = P.counts[(int64_t)P.n_groups * E + e];
+    }
+  } else {
+    for (int e = (int)threadIdx.x; e < E; e += kThreads) before[e] = total[e] = 0;
+    __syncthreads();
+    const int share = E < kThreads ? kThreads / E : 1, my = (int)threadIdx.x / E;
+    for (int e = share > 1 ? (int)threadIdx.x - my * E : (int)threadIdx.x; e < E && my < share; e += share > 1 ? E : kThreads) {
+      uint32_t all = 0, mine = 0;
+#pragma unroll 8
+      for (int i = share > 1 ? my : 0; i < P.n_groups; i += share) {
+        const uint32_t c = P.counts[i * E + e];
+        all += c;
+        mine += i < g ? c : 0;
+      }
+      atomicAdd(&total[e], all);
+      atomicAdd(&before[e], mine);
     }
   }
+  __syncthreads();
 }
 
 // Token t's row to the rows of its slots, lane j's `slot` the row of slot j;
-// `c`, `step`: this lane's chunks.
-template <typename T>
-__device__ __forceinline__ void copy_row(const DispatchParams &P, int64_t t, int64_t c, int64_t step, int slot) {
+// this lane takes chunks `at`, at + step, ...
+template <typename T, bool kStream>
+__device__ __forceinline__ void copy_row(const DispatchParams &P, int64_t t, int64_t at, int64_t step, int slot) {
+  constexpr int E = Chunk<T>::kElems;
   const T *x = static_cast<const T *>(P.x) + t * P.x_stride;
   T *out = static_cast<T *>(P.rows);
-  const int64_t chunks = (P.width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
-  for (; c < chunks; c += step) {
-    const auto v = load_chunk<T>(x, c, P.width);
-    for (int j = 0; j < P.k; ++j) {
-      const int row = __builtin_amdgcn_readlane(slot, j);
-      if (row >= 0) store_chunk<T>(out + (int64_t)row * P.rows_stride, c, P.width, v);
+  const int64_t chunks = P.width / E;
+  const uint64_t set = __ballot(slot >= 0);
+  each_chunk<2>(at, chunks, step, [&](auto us, int64_t c) {
+    constexpr int U = decltype(us)::value;
+    typename Chunk<T>::vec v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load<false>(x + (c + u * step) * E);
+    for (uint64_t left = set; left; left &= left - 1) {
+      T *row = out + __builtin_amdgcn_readlane(slot, __builtin_ctzll(left)) * P.rows_stride;
+#pragma unroll
+      for (int u = 0; u < U; ++u) store<kStream>(row + (c + u * step) * E, v[u]);
+    }
+  });
+  const int64_t i = chunks * E + at;               // the elements behind the last whole chunk
+  if (at < E && i < P.width) {
+    const T v = x[i];
+    for (uint64_t left = set; left; left &= left - 1)
+      out[__builtin_amdgcn_readlane(slot, __builtin_ctzll(left)) * P.rows_stride + i] = v;
+  }
+}
+
+template <typename T, bool kStream>
+__global__ void __launch_bounds__(kThreads) dispatch_kernel(DispatchParams P) {
+  extern __shared__ uint32_t lds[];
+  const int E = P.n_experts;
+  uint32_t *hist = lds, *total = hist + kWaves * E, *start = total + E, *before = start + E + 1;
+  int32_t *rows = reinterpret_cast<int32_t *>(before + E);
+  const int wave = wave_index(), lane = lane_index();
+  const int g = (int)blockIdx.x / P.parts, part = (int)blockIdx.x - g * P.parts;
+  const int64_t first = (int64_t)g * P.group;
+  int id[kBatches], row[kBatches];
+  load_ids(P, g, wave, lane, id);
+  count_waves(P, id, wave, hist, total);
+  if (P.n_groups > 1) sum_groups(P, g, before, total);
+  expert_starts(E, total, start, wave, lane);
+  if (P.n_groups > 1) {
+    for (int e = (int)threadIdx.x; e < E; e += kThreads) before[e] += start[e];
+    __syncthreads();
+  }
+  rank_slots(P, id, wave, lane, hist, P.n_groups > 1 ? before : start, row);
+  if (blockIdx.x == 0)
+    for (int e = (int)threadIdx.x; e <= E; e += kThreads) P.off[e] = (int32_t)start[e];
+#pragma unroll
+  for (int b = 0; b < kBatches; ++b) {
+    const int i = (wave * kBatches + b) * kWave + lane;
+    rows[i] = row[b];
+    if (part == 0 && i < P.group && first + i < P.n_slots) {
+      P.pos[first + i] = row[b];
+      if (row[b] >= 0) P.perm[row[b]] = (int32_t)((first + i) / P.k);
     }
   }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kSmallWaves *kWave) dispatch_small_kernel(DispatchParams P, int64_t spans) {
-  extern __shared__ uint32_t lds[];
-  uint32_t *hist = lds, *total = hist + kSmallWaves * P.n_experts, *start = total + P.n_experts;
-  int32_t *rows = reinterpret_cast<int32_t *>(start + P.n_experts + 1);
-  const int wave = wave_index(), lane = lane_index();
-  int id[kBatches], row[kBatches];
-  load_ids(P, 0, wave, lane, id);
-  count_waves<kSmallWaves>(P, id, wave, hist, total);
-  expert_starts(P.n_experts, total, start, wave, lane);
-  rank_slots<kSmallWaves>(P, id, wave, lane, hist, start, row);
-  if (blockIdx.x == 0) {
-    store_ranks(P, 0, wave, lane, row);
-    for (int e = (int)threadIdx.x; e <= P.n_experts; e += kSmallWaves * kWave) P.off[e] = (int32_t)start[e];
-  }
   if (!P.x) return;
-#pragma unroll
-  for (int b = 0; b < kBatches; ++b) rows[(wave * kBatches + b) * kWave + lane] = row[b];
   __syncthreads();
-  // a token's row is copied by `spans` waves
-  const int64_t tokens = P.n_slots / P.k, waves = (int64_t)gridDim.x * kSmallWaves;
-  for (int64_t u = (int64_t)blockIdx.x * kSmallWaves + wave; u < tokens * spans; u += waves) {
-    const int64_t t = u / spans;
-    copy_row<T>(P, t, (u - t * spans) * kWave + lane, spans * kWave, lane < P.k ? rows[t * P.k + lane] : -1);
+  // the group's tokens, `spans` waves each, over the waves of its workgroups
+  const int64_t left = P.n_slots - first;
+  const int tokens = (int)(left < P.group ? left : P.group) / P.k, spans = (int)P.spans, waves = P.parts * kWaves;
+  for (int u = part * kWaves + wave; u < tokens * spans; u += waves) {
+    const int t = u / spans;
+    copy_row<T, kStream>(P, first / P.k + t, (u - t * spans) * kWave + lane, P.spans * kWave,
+                         lane < P.k ? rows[t * P.k + lane] : -1);
   }
 }
 
-__global__ void __launch_bounds__(kGroupWaves *kWave) count_kernel(DispatchParams P) {
+// A wave takes a token, or one of `spans` parts of its row.
+template <typename T, bool kStream>
+__global__ void __launch_bounds__(kThreads) copy_kernel(DispatchParams P) {
+  const int64_t u = (int64_t)blockIdx.x * kWaves + wave_index(), t = u / P.spans;
+  if (t >= P.n_slots / P.k) return;
+  const int lane = lane_index();
+  copy_row<T, kStream>(P, t, (u - t * P.spans) * kWave + lane, P.spans * kWave, lane < P.k ? P.pos[t * P.k + lane] : -1);
+}
+
+__global__ void __launch_bounds__(kThreads) count_kernel(DispatchParams P) {
   extern __shared__ uint32_t lds[];
   const int wave = wave_index(), lane = lane_index();
   int id[kBatches];
-  load_ids(P, (int64_t)blockIdx.x * kGroupSlots, wave, lane, id);
-  for (int e = (int)threadIdx.x; e < P.n_experts; e += kGroupWaves * kWave) lds[e] = 0;
+  load_ids(P, (int)blockIdx.x, wave, lane, id);
+  for (int e = (int)threadIdx.x; e < P.n_experts; e += kThreads) lds[e] = 0;
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < kBatches; ++b)
     if (id[b] >= 0) atomicAdd(&lds[id[b]], 1u);
   __syncthreads();
-  for (int e = (int)threadIdx.x; e < P.n_experts; e += kGroupWaves * kWave)
-    P.counts[(int64_t)blockIdx.x * P.n_experts + e] = lds[e];
+  for (int e = (int)threadIdx.x; e < P.n_experts; e += kThreads) P.counts[(int64_t)blockIdx.x * P.n_experts + e] = lds[e];
 }
 
-__global__ void __launch_bounds__(kGroupWaves *kWave) rank_kernel(DispatchParams P) {
-  extern __shared__ uint32_t lds[];
-  const int E = P.n_experts;
-  uint32_t *hist = lds, *total = hist + kGroupWaves * E, *start = total + E, *before = start + E + 1;
-  const int wave = wave_index(), lane = lane_index();
-  const int64_t first = (int64_t)blockIdx.x * kGroupSlots;
-  int id[kBatches], row[kBatches];
-  load_ids(P, first, wave, lane, id);
-  count_waves<kGroupWaves>(P, id, wave, hist, total);
-  for (int e = (int)threadIdx.x; e < E; e += kGroupWaves * kWave) {
-    uint32_t all = 0, mine = 0;
-    for (int g = 0; g < P.n_groups; ++g) {
-      const uint32_t c = P.counts[(int64_t)g * E + e];
-      all += c;
-      mine += g < (int)blockIdx.x ? c : 0;
+// counts[g][e] to the sum over the groups before g, in place, and
+// counts[n_groups][e] the sum of all; a wave per expert, a lane per group.
+__global__ void __launch_bounds__(kThreads) sum_kernel(DispatchParams P) {
+  const int e = (int)blockIdx.x * kWaves + wave_index(), lane = lane_index();
+  if (e >= P.n_experts) return;
+  uint32_t before = 0;
+  for (int g0 = 0; g0 < P.n_groups; g0 += kWave) {
+    const int g = g0 + lane;
+    uint32_t *at = P.counts + (int64_t)g * P.n_experts + e;
+    const uint32_t c = g < P.n_groups ? *at : 0;
+    uint32_t sum = c;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const uint32_t up = (uint32_t)__shfl_up((int)sum, d);
+      sum += lane >= d ? up : 0;
     }
-    total[e] = all;
-    before[e] = mine;
+    if (g < P.n_groups) *at = before + sum - c;
+    before += (uint32_t)__builtin_amdgcn_readlane((int)sum, kWave - 1);
   }
-  __syncthreads();
-  expert_starts(E, total, start, wave, lane);
-  for (int e = (int)threadIdx.x; e <= E; e += kGroupWaves * kWave) {
-    if (blockIdx.x == 0) P.off[e] = (int32_t)start[e];
-    if (e < E) before[e] += start[e];
-  }
-  __syncthreads();
-  rank_slots<kGroupWaves>(P, id, wave, lane, hist, before, row);
-  store_ranks(P, first, wave, lane, row);
+  if (lane == 0) P.counts[(int64_t)P.n_groups * P.n_experts + e] = before;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(256) copy_kernel(DispatchParams P) {
-  const int64_t t = (int64_t)blockIdx.x * 4 + wave_index();
-  if (t >= P.n_slots / P.k) return;
-  const int lane = lane_index();
-  copy_row<T>(P, t, lane, kWave, lane < P.k ? P.pos[t * P.k + lane] : -1);
+int32_t group_of(int32_t k) { return kGroupSlots / k * k; }
+int64_t groups_of(int64_t slots, int32_t k) { return (slots + group_of(k) - 1) / group_of(k); }
+int64_t counts_of(int64_t slots, int32_t k, int32_t n_experts) {
+  const int64_t groups = groups_of(slots, k);
+  return groups <= 1 ? 0 : (groups + 1) * n_experts * (int64_t)sizeof(uint32_t);
 }
-
-int64_t groups_of(int64_t slots) { return slots <= kSmallSlots ? 0 : (slots + kGroupSlots - 1) / kGroupSlots; }
 
 bfs_status check_sizes(const char *what, int64_t n_tokens, int32_t k, int32_t n_experts) {
   if (n_tokens < 0 || k < 1 || n_experts < 1) return fail(BFS_E_INVALID, std::string(what) + ": a negative or zero size");
@@ -255,7 +301,7 @@ bfs_status bfs_moe_dispatch_workspace(int64_t n_tokens, int32_t k, int32_t n_exp
     bfs_status st = check_sizes("moe_dispatch_workspace", n_tokens, k, n_experts);
     if (st != BFS_OK) return st;
     if (!bytes) return fail(BFS_E_INVALID, "moe_dispatch_workspace: null result");
-    *bytes = groups_of(n_tokens * k) * n_experts * (int64_t)sizeof(uint32_t);
+    *bytes = counts_of(n_tokens * k, k, n_experts);
     return BFS_OK;
   });
 }
@@ -267,7 +313,7 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
   return entry([&]() -> bfs_status {
     bfs_status st = check_sizes("moe_dispatch", n_tokens, k, n_experts);
     if (st != BFS_OK) return st;
-    const int64_t slots = n_tokens * k, groups = groups_of(slots), need = groups * n_experts * (int64_t)sizeof(uint32_t);
+    const int64_t slots = n_tokens * k, groups = groups_of(slots, k), need = counts_of(slots, k, n_experts);
     if (!expert_off || (slots > 0 && (!experts || !perm || !pos))) return fail(BFS_E_INVALID, "moe_dispatch: null buffer");
     if ((x == nullptr) != (rows == nullptr) && slots > 0)
       return fail(BFS_E_INVALID, "moe_dispatch: x and rows are given together");
@@ -291,32 +337,38 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
     P.k = k;
     P.n_experts = n_experts;
     P.n_groups = (int32_t)groups;
+    P.group = group_of(k);
+    P.parts = 1;
     while ((1 << P.bits) < n_experts) ++P.bits;
     auto copy = [&](auto t) -> bfs_status {
       using T = decltype(t);
-      if (groups == 0) {
-        const size_t lds = ((kSmallWaves + 2) * (size_t)n_experts + 1 + kSmallSlots) * sizeof(uint32_t);
-        int64_t spans = 1, blocks = 1;
-        if (P.x) {
-          // four chunks for a lane at most while that leaves compute units idle
-          const int64_t chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
-          const int64_t most = (chunks + kWave - 1) / kWave, wanted = (1024 + n_tokens - 1) / n_tokens;
-          spans = most < wanted ? most : wanted;
-          blocks = (n_tokens * spans + kSmallWaves - 1) / kSmallWaves;
-          blocks = blocks < 512 ? blocks : 512;
-        }
-        return launch("moe_dispatch", dispatch_small_kernel<T>, blocks, kSmallWaves * kWave, lds, stream, P, spans);
-      }
-      const size_t lds = ((kGroupWaves + 3) * (size_t)n_experts + 1) * sizeof(uint32_t);
-      bfs_status s = launch("moe_dispatch", count_kernel, groups, kGroupWaves * kWave, n_experts * sizeof(uint32_t), stream, P);
-      if (s == BFS_OK && lds > 64 * 1024) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(rank_kernel),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        if (e != hipSuccess) s = fail(BFS_E_DEVICE, std::string("moe_dispatch: attribute: ") + hipGetErrorString(e));
-      }
-      if (s == BFS_OK) s = launch("moe_dispatch", rank_kernel, groups, kGroupWaves * kWave, lds, stream, P);
-      if (s == BFS_OK && P.x) s = launch("moe_dispatch", copy_kernel<T>, (n_tokens + 3) / 4, 256, 0, stream, P);
-      return s;
+      bfs_status s = BFS_OK;
+      if (groups > 1) s = launch("moe_dispatch", count_kernel, groups, kThreads, n_experts * sizeof(uint32_t), stream, P);
+      if (s == BFS_OK && groups > 1 && groups * n_experts > kSumEntries)
+        s = launch("moe_dispatch", sum_kernel, (n_experts + kWaves - 1) / kWaves, kThreads, 0, stream, P);
+      if (s != BFS_OK) return s;
+      const size_t lds = ((kWaves + 3) * (size_t)n_experts + 1 + kGroupSlots) * sizeof(uint32_t);
+      const int64_t all = groups > 0 ? groups : 1;
+      if (!P.x) return launch("moe_dispatch", dispatch_kernel<T, false>, all, kThreads, lds, stream, P);
+      // two waves for a row of four steps and more (32768 tokens of 4096 bf16 to
+      // two experts each: 156 us, with one 162), one step for each wave where the
+      // tokens are fewer than 512
+      const int64_t steps = (width + kWave * Chunk<T>::kElems - 1) / (kWave * Chunk<T>::kElems);
+      const int64_t wanted = (511 + n_tokens) / n_tokens, least = steps >= 4 ? 2 : 1;
+      P.spans = wanted < least ? least : wanted < steps ? wanted : steps;
+      const bool stream_rows = (k + 1) * n_tokens * width * (int64_t)sizeof(T) >= kStreamFrom;
+      const int64_t in_group = (n_tokens < P.group / k ? n_tokens : P.group / k) * P.spans;
+      P.parts = (int32_t)((in_group + kWaves - 1) / kWaves);
+      if (all * P.parts <= kBlocks)
+        return launch("moe_dispatch", stream_rows ? dispatch_kernel<T, true> : dispatch_kernel<T, false>, all * P.parts, kThreads,
+                      lds, stream, P);
+      P.parts = 1;
+      P.x = nullptr;
+      s = launch("moe_dispatch", dispatch_kernel<T, false>, all, kThreads, lds, stream, P);
+      P.x = x;
+      if (s != BFS_OK) return s;
+      return launch("moe_dispatch", stream_rows ? copy_kernel<T, true> : copy_kernel<T, false>,
+                    (n_tokens * P.spans + kWaves - 1) / kWaves, kThreads, 0, stream, P);
     };
     // rows are moved, not computed with: the element's size decides
     switch (dtype) {

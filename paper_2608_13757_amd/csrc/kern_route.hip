@@ -18,7 +18,6 @@
 // Logits are compared as unsigned keys in the order of the floats, -0 as +0,
 // NaN above everything; the softmax is in fp32 whatever the logits' type.
 #include <cmath>
-#include <tuple>
 
 #include "op_common.h"
 

@@ -6,6 +6,8 @@
 
 #include <cstdint>
 #include <string>
+#include <tuple>
+#include <type_traits>
 
 #include "bfs_internal.h"
 
@@ -53,6 +55,47 @@ __device__ __forceinline__ void store_chunk(T *row, int64_t c, int64_t n, typena
     for (int i = 0; i < E; ++i)
       if (c * E + i < n) row[c * E + i] = v[i];
   }
+}
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+// f(U, c) for this lane's chunks c, c + step, ..., U of them at once, then with
+// U / 2.
+template <int U, typename F>
+__device__ __forceinline__ void each_chunk(int64_t c, int64_t chunks, int64_t step, F f) {
+  for (; c + (U - 1) * step < chunks; c += U * step) f(Int<U>{}, c);
+  if constexpr (U > 1) each_chunk<U / 2>(c, chunks, step, f);
+}
+
+// Bytes that a call moves from which its accesses are nontemporal: what does
+// not fit the L2s twice over is not worth keeping there, and the last-level
+// cache serves reads and writes faster when they pass it by (16384 tokens of 8
+// rows of 2048 bf16 combined: 120 us with plain accesses, 103 with nontemporal
+// loads, 100 with both; 64 rows of 8192, 9 MB: 3.3 and 3.7 us).
+constexpr int64_t kStreamFrom = 64 << 20;
+
+// An access to 16 bytes, nontemporal with kStream.
+template <bool kStream, typename T>
+__device__ __forceinline__ typename Chunk<T>::vec load(const T *p) {
+  auto q = reinterpret_cast<const typename Chunk<T>::vec *>(p);
+  return kStream ? __builtin_nontemporal_load(q) : *q;
+}
+
+template <bool kStream, typename T>
+__device__ __forceinline__ void store(T *p, typename Chunk<T>::vec v) {
+  auto q = reinterpret_cast<typename Chunk<T>::vec *>(p);
+  if (kStream) __builtin_nontemporal_store(v, q);
+  else *q = v;
+}
+
+// Waves that share a token's row of `most` steps of a wave: one round of four
+// steps for each (32768 tokens, 2 rows of 4096 bf16 combined: 129 us, with one
+// wave for all eight steps 138), one step where that leaves the compute units
+// without 4096 waves.
+inline int64_t spans_of(int64_t most, int64_t n_tokens) {
+  const int64_t rounds = (most + 3) / 4, wanted = (4095 + n_tokens) / n_tokens;
+  return wanted < rounds ? rounds : wanted < most ? wanted : most;
 }
 
 // Lane i's value from lane i - s of its row of 16 lanes, the row as a ring.

@@ -21,7 +21,7 @@ from .bfs import E_INVALID, OK, BfsError
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOE_RENORMALIZE = 1
-DISPATCH_ONE_LAUNCH = 1024       # slots up to which the dispatch needs no workspace
+DISPATCH_ONE_GROUP = 1024        # slots of one group: at most one needs no workspace
 
 
 def _refuse(name, what):
@@ -174,9 +174,9 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
     t, k = shape
     slots = t * k
     _dense(name, "experts", experts, device, shape, torch.int32)
-    one_launch = slots <= DISPATCH_ONE_LAUNCH
+    one_group = k and slots <= DISPATCH_ONE_GROUP // k * k
     handle = _stream(name, stream, device, perm is not None and expert_off is not None and pos is not None
-                     and (x is None or rows is not None) and (one_launch or workspace is not None))
+                     and (x is None or rows is not None) and (one_group or workspace is not None))
     if perm is None:
         perm = experts.new_empty(slots)
     else:
@@ -203,7 +203,7 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         x_ptr, rows_ptr = x.data_ptr(), rows.data_ptr()
     elif rows is not None:
         _refuse(name, "rows without x")
-    if not one_launch:
+    if not one_group:
         if workspace is None:
             workspace = experts.new_empty(moe_dispatch_workspace(t, k, n_experts), dtype=torch.uint8)
         elif workspace.get_device() != device or not workspace.is_contiguous():

@@ -125,9 +125,11 @@ def test_nothing_to_do():
 def test_workspaces():
     torch = pytest.importorskip("torch")
     from paper_2608_13757_amd import GradSet, moe_dispatch_workspace
-    from paper_2608_13757_amd.ops import DISPATCH_ONE_LAUNCH
-    assert moe_dispatch_workspace(1, 1, 64) == 0 and moe_dispatch_workspace(DISPATCH_ONE_LAUNCH, 1, 64) == 0
-    assert moe_dispatch_workspace(DISPATCH_ONE_LAUNCH + 1, 1, 64) > 0
+    from paper_2608_13757_amd.ops import DISPATCH_ONE_GROUP
+    for k in (1, 2, 3, 7, 64):
+        most = DISPATCH_ONE_GROUP // k
+        assert moe_dispatch_workspace(0, k, 64) == 0 and moe_dispatch_workspace(most, k, 64) == 0
+        assert moe_dispatch_workspace(most + 1, k, 64) > 0
     assert moe_dispatch_workspace(32768, 2, 64) > 0
     for bad in ((-1, 1, 4), (4, 0, 4), (4, 1, 0)):
         with pytest.raises(BfsError) as e:
