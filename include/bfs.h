@@ -385,6 +385,7 @@ bfs_status bfs_run_status(const bfs_plan *plan, struct ihipStream_t *stream);
  * in elements: an output's at least the width, an input's anything from 0
  * (one row for all).  Rows need no more than their element's alignment.
  * Outputs must not overlap inputs or each other except where it is said.
+ * At most 2^24 - 1 tokens.
  */
 typedef enum { BFS_DTYPE_F32 = 0, BFS_DTYPE_BF16 = 1, BFS_DTYPE_F16 = 2 } bfs_dtype;
 
@@ -424,7 +425,7 @@ bfs_status bfs_moe_route_grad(const void *logits, int32_t dtype, int64_t n_token
  *   rows        NULL with x NULL, or [n_tokens * k][width]: x[token] of each row
  * perm and expert_off are buffers [1] and [2] of the MoE family.  Entries of
  * perm and rows behind the last row are left as they were.  k <= 64,
- * n_experts <= 1024, fewer than 2^31 slots.  workspace: device memory of
+ * n_experts <= 1024.  workspace: device memory of
  * bfs_moe_dispatch_workspace bytes (may be 0: NULL then), free to reuse when
  * the work has completed; calls that overlap need one each.
  */

@@ -287,8 +287,8 @@ int64_t counts_of(int64_t slots, int32_t k, int32_t n_experts) {
 
 bfs_status check_sizes(const char *what, int64_t n_tokens, int32_t k, int32_t n_experts) {
   if (n_tokens < 0 || k < 1 || n_experts < 1) return fail(BFS_E_INVALID, std::string(what) + ": a negative or zero size");
-  if (n_experts > kMaxExperts || k > kMaxK || n_tokens > ((int64_t)1 << 31) / k - 1)
-    return fail(BFS_E_RESOURCE, std::string(what) + ": at most 1024 experts, 64 per token and 2^31 - 1 slots");
+  if (n_experts > kMaxExperts || k > kMaxK || n_tokens > kMaxTokens)
+    return fail(BFS_E_RESOURCE, std::string(what) + ": at most 1024 experts, 64 per token and 2^24 - 1 tokens");
   return BFS_OK;
 }
 

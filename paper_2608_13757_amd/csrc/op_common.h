@@ -16,6 +16,7 @@ namespace bfsop {
 using bfs::fail;
 
 constexpr int kWave = 64;
+constexpr int64_t kMaxTokens = ((int64_t)1 << 24) - 1;
 
 // 16 bytes of a row.  Rows start at any element (odd widths, views), so the
 // alignment is the element's; global accesses of four words need no more.
@@ -68,12 +69,12 @@ __device__ __forceinline__ void each_chunk(int64_t c, int64_t chunks, int64_t st
   if constexpr (U > 1) each_chunk<U / 2>(c, chunks, step, f);
 }
 
-// Bytes that a call moves from which its accesses are nontemporal: what does
-// not fit the L2s twice over is not worth keeping there, and the last-level
-// cache serves reads and writes faster when they pass it by (16384 tokens of 8
-// rows of 2048 bf16 combined: 120 us with plain accesses, 103 with nontemporal
-// loads, 100 with both; 64 rows of 8192, 9 MB: 3.3 and 3.7 us).
-constexpr int64_t kStreamFrom = 64 << 20;
+// Bytes that a call moves from which its accesses are nontemporal: so much is
+// not worth keeping in the caches, and memory serves reads and writes faster
+// when they pass them by (16384 tokens of 8 rows of 2048 bf16 combined, 605 MB:
+// 120 us with plain accesses, 103 with nontemporal loads, 100 with both; 70 MB:
+// 13.4 and 14.9; 9 MB: 3.3 and 3.7).
+constexpr int64_t kStreamFrom = 96 << 20;
 
 // An access to 16 bytes, nontemporal with kStream.
 template <bool kStream, typename T>
@@ -113,9 +114,9 @@ __device__ __forceinline__ uint32_t group_reduce(uint32_t x, F f) {
   x = f(x, ror16<4>(x));
   x = f(x, ror16<2>(x));
   x = f(x, ror16<1>(x));
-  if (G == 64) {
-    x = f(x, (uint32_t)__shfl_xor((int)x, 16));
-    x = f(x, (uint32_t)__shfl_xor((int)x, 32));
+  if (G == 64) {                                   // the four rows' results, in scalar registers
+    auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); };
+    x = f(f(row(0), row(16)), f(row(32), row(48)));
   }
   return x;
 }
@@ -150,6 +151,7 @@ __device__ __forceinline__ int lane_index() { return (int)(threadIdx.x & 63u); }
 
 template <typename... P, typename... A>
 bfs_status launch(const char *what, void (*kernel)(P...), int64_t blocks, int threads, size_t lds, void *stream, A... a) {
+  if (blocks * threads >= (int64_t)1 << 32) return fail(BFS_E_RESOURCE, std::string(what) + ": more than 2^32 - 1 threads");
   std::tuple<P...> params(static_cast<P>(a)...);
   void *ptrs[sizeof...(P)];
   std::apply([&](auto &...p) {
