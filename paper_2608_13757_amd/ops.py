@@ -8,6 +8,10 @@ before anything is launched.  Outputs that are not given are allocated on the
 current stream.  ``stream``: a torch stream or handle, None the current one;
 on another stream than the current one every output (and the workspace) has to
 be given, since an allocation belongs to the stream that it was made on.
+
+Calls of a few tokens are bound by the host (2.9 us of a call are the launch),
+so the checks stand in the calls themselves; the functions they call say what
+is wrong.
 """
 from __future__ import annotations
 
@@ -22,11 +26,7 @@ from .bfs import E_INVALID, OK, BfsError
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOE_RENORMALIZE = 1
 DISPATCH_ONE_GROUP = 1024        # slots of one group: at most one needs no workspace
-
-
-def _refuse(name, what):
-    raise BfsError(E_INVALID, f"{name}: {what}")
-
+_I32, _F32 = torch.int32, torch.float32
 
 # The current device and its current stream's handle, by the bindings that
 # torch.cuda's functions wrap (which take most of a microsecond together).
@@ -34,56 +34,31 @@ _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_devic
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: bfs._stream_handle(None))
 
 
-def _dtype(name, t):
-    code = DTYPES.get(t.dtype)
-    if code is None:
-        _refuse(name, f"element type {t.dtype} (float32, bfloat16 and float16 are supported)")
-    return code
+def _refuse(name, what):
+    raise BfsError(E_INVALID, f"{name}: {what}")
 
 
-def _first(name, what, t):
-    """The device of a call's first tensor, which must be the current one."""
-    device = t.get_device()
-    if device < 0 or device != _device():
-        _refuse(name, f"{what} must be on the current device")
-    return device
+def _refuse_matrix(name, what, t):
+    _refuse(name, f"{what} must be a matrix on the current device with unit stride in its rows, not {tuple(t.shape)} with "
+                  f"strides {t.stride()} on {t.device}")
 
 
-def _matrix(name, what, t, device, out=False):
-    """(rows, width, stride between rows) of a tensor of two dimensions whose
-    rows have unit stride; an output's rows must not overlap."""
-    size = t.shape
-    if len(size) != 2 or t.get_device() != device:
-        _refuse(name, f"{what} must have two dimensions and be on the current device, not {tuple(size)}")
-    n, width = size
-    stride, unit = t.stride()
-    if unit != 1 and width > 1:
-        _refuse(name, f"{what} must have unit stride in its rows")
-    if n <= 1:
-        return n, width, width
-    if out and stride < width:
-        _refuse(name, f"{what} has rows that overlap")
-    return n, width, stride
+def _refuse_like(name, what, t, shape, dtype):
+    _refuse(name, f"{what} must be {dtype} of shape {tuple(shape)} on the current device with unit stride in rows that do "
+                  f"not overlap, not {t.dtype} {tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _matrix_like(name, what, t, device, shape, dtype, out=False):
-    """The stride between the rows of a matrix of a given shape and type."""
-    if t.dtype is not dtype or t.shape != shape:
-        _refuse(name, f"{what} must be {dtype} of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
-    return _matrix(name, what, t, device, out)[2]
+def _refuse_dense(name, what, t, shape, dtype):
+    _refuse(name, f"{what} must be contiguous {dtype} of shape {tuple(shape)} on the current device, not {t.dtype} "
+                  f"{tuple(t.shape)} with strides {t.stride()} on {t.device}")
 
 
-def _dense(name, what, t, device, shape, dtype):
-    """A contiguous tensor of a given shape and type."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
-        _refuse(name, f"{what} must be contiguous {dtype} of shape {tuple(shape)} on the current device, not {t.dtype} "
-                      f"{tuple(t.shape)}")
+def _refuse_type(name, what, t):
+    _refuse(name, f"{what} of type {t.dtype} (float32, bfloat16 and float16 are supported)")
 
 
 def _stream(name, stream, device, given):
-    """Handle of the stream; ``given``: whether nothing has to be allocated."""
-    if stream is None:
-        return _raw_stream(device)
+    """Handle of a stream; ``given``: whether nothing has to be allocated."""
     handle = bfs._stream_handle(stream)
     if not given and handle != _raw_stream(device):
         _refuse(name, "on another stream than the current one every output and the workspace must be given")
@@ -103,23 +78,31 @@ def moe_route(logits, k, *, renormalize=True, experts=None, weights=None, stream
     A logit of -inf masks its expert; slots left without one hold -1 and
     weight 0."""
     name = "moe_route"
-    device = _first(name, "logits", logits)
-    t, e, stride = _matrix(name, "logits", logits, device)
+    device, size = logits.get_device(), logits.shape
+    if device < 0 or device != _device() or len(size) != 2:
+        _refuse_matrix(name, "logits", logits)
+    t, e = size
+    stride, unit = logits.stride()
+    if unit != 1 and e > 1:
+        _refuse_matrix(name, "logits", logits)
+    dtype = DTYPES.get(logits.dtype)
+    if dtype is None:
+        _refuse_type(name, "logits", logits)
     if k < 1:
         _refuse(name, f"k = {k}")
-    handle = _stream(name, stream, device, experts is not None and weights is not None)
+    handle = _raw_stream(device) if stream is None else _stream(name, stream, device, experts is not None and weights is not None)
     shape = (t, k)
     if experts is None:
-        experts = logits.new_empty(shape, dtype=torch.int32)
-    else:
-        _dense(name, "experts", experts, device, shape, torch.int32)
+        experts = logits.new_empty(shape, dtype=_I32)
+    elif experts.dtype is not _I32 or experts.shape != shape or experts.get_device() != device or not experts.is_contiguous():
+        _refuse_dense(name, "experts", experts, shape, _I32)
     if weights is None:
-        weights = logits.new_empty(shape, dtype=torch.float32)
-    else:
-        _dense(name, "weights", weights, device, shape, torch.float32)
+        weights = logits.new_empty(shape, dtype=_F32)
+    elif weights.dtype is not _F32 or weights.shape != shape or weights.get_device() != device or not weights.is_contiguous():
+        _refuse_dense(name, "weights", weights, shape, _F32)
     status = (bfs._lib or bfs.lib()).bfs_moe_route(
-        logits.data_ptr(), _dtype(name, logits), t, e, stride, k, MOE_RENORMALIZE if renormalize else 0,
-        experts.data_ptr(), weights.data_ptr(), handle)
+        logits.data_ptr(), dtype, t, e, stride, k, MOE_RENORMALIZE if renormalize else 0, experts.data_ptr(),
+        weights.data_ptr(), handle)
     if status:
         bfs._check(status)
     return experts, weights
@@ -129,20 +112,34 @@ def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logi
     """The gradient of the logits (of their type) for the gradient of the
     router's weights; ``experts`` and ``renormalize`` as the router had them."""
     name = "moe_route_grad"
-    device = _first(name, "logits", logits)
-    t, e, stride = _matrix(name, "logits", logits, device)
+    device, size = logits.get_device(), logits.shape
+    if device < 0 or device != _device() or len(size) != 2:
+        _refuse_matrix(name, "logits", logits)
+    t, e = size
+    stride, unit = logits.stride()
+    if unit != 1 and e > 1:
+        _refuse_matrix(name, "logits", logits)
+    dtype = DTYPES.get(logits.dtype)
+    if dtype is None:
+        _refuse_type(name, "logits", logits)
     k = experts.shape[-1]
     shape = (t, k)
-    _dense(name, "experts", experts, device, shape, torch.int32)
-    _dense(name, "grad_weights", grad_weights, device, shape, torch.float32)
-    handle = _stream(name, stream, device, grad_logits is not None)
+    if experts.dtype is not _I32 or experts.shape != shape or experts.get_device() != device or not experts.is_contiguous():
+        _refuse_dense(name, "experts", experts, shape, _I32)
+    if (grad_weights.dtype is not _F32 or grad_weights.shape != shape or grad_weights.get_device() != device
+            or not grad_weights.is_contiguous()):
+        _refuse_dense(name, "grad_weights", grad_weights, shape, _F32)
+    handle = _raw_stream(device) if stream is None else _stream(name, stream, device, grad_logits is not None)
     if grad_logits is None:
-        grad_logits, out_stride = logits.new_empty((t, e)), e
-    else:
-        out_stride = _matrix_like(name, "grad_logits", grad_logits, device, (t, e), logits.dtype, True)
+        grad_logits = logits.new_empty(size)
+    elif grad_logits.dtype is not logits.dtype or grad_logits.shape != size or grad_logits.get_device() != device:
+        _refuse_like(name, "grad_logits", grad_logits, size, logits.dtype)
+    out_stride, unit = grad_logits.stride()
+    if (unit != 1 and e > 1) or (out_stride < e and t > 1):
+        _refuse_like(name, "grad_logits", grad_logits, size, logits.dtype)
     status = (bfs._lib or bfs.lib()).bfs_moe_route_grad(
-        logits.data_ptr(), _dtype(name, logits), t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
-        MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride, handle)
+        logits.data_ptr(), dtype, t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
+        MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride if t > 1 else e, handle)
     if status:
         bfs._check(status)
     return grad_logits
@@ -165,41 +162,52 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
     without x [T, width].  Entries of perm and rows behind the last row are
     left as they were."""
     name = "moe_dispatch"
-    device = _first(name, "experts", experts)
-    shape = experts.shape
-    if len(shape) != 2:
-        _refuse(name, "experts must have two dimensions")
+    device, shape = experts.get_device(), experts.shape
+    if device < 0 or device != _device() or len(shape) != 2 or experts.dtype is not _I32 or not experts.is_contiguous():
+        _refuse(name, f"experts must be a contiguous int32 matrix on the current device, not {experts.dtype} {tuple(shape)}")
     if n_experts < 1:
         _refuse(name, f"n_experts = {n_experts}")
     t, k = shape
     slots = t * k
-    _dense(name, "experts", experts, device, shape, torch.int32)
     one_group = k and slots <= DISPATCH_ONE_GROUP // k * k
-    handle = _stream(name, stream, device, perm is not None and expert_off is not None and pos is not None
-                     and (x is None or rows is not None) and (one_group or workspace is not None))
+    handle = _raw_stream(device) if stream is None else _stream(
+        name, stream, device, perm is not None and expert_off is not None and pos is not None
+        and (x is None or rows is not None) and (one_group or workspace is not None))
     if perm is None:
         perm = experts.new_empty(slots)
-    else:
-        _dense(name, "perm", perm, device, (slots,), torch.int32)
+    elif perm.dtype is not _I32 or perm.shape != (slots,) or perm.get_device() != device or not perm.is_contiguous():
+        _refuse_dense(name, "perm", perm, (slots,), _I32)
     if expert_off is None:
         expert_off = experts.new_empty(n_experts + 1)
-    else:
-        _dense(name, "expert_off", expert_off, device, (n_experts + 1,), torch.int32)
+    elif (expert_off.dtype is not _I32 or expert_off.shape != (n_experts + 1,) or expert_off.get_device() != device
+          or not expert_off.is_contiguous()):
+        _refuse_dense(name, "expert_off", expert_off, (n_experts + 1,), _I32)
     if pos is None:
         pos = experts.new_empty(shape)
-    else:
-        _dense(name, "pos", pos, device, shape, torch.int32)
+    elif pos.dtype is not _I32 or pos.shape != shape or pos.get_device() != device or not pos.is_contiguous():
+        _refuse_dense(name, "pos", pos, shape, _I32)
     x_ptr = rows_ptr = ws_ptr = None
     dtype = width = x_stride = rows_stride = ws_bytes = 0
     if x is not None:
-        n, width, x_stride = _matrix(name, "x", x, device)
-        dtype = _dtype(name, x)
-        if n != t:
-            _refuse(name, f"x has {n} rows for {t} tokens")
+        size = x.shape
+        if x.get_device() != device or len(size) != 2 or size[0] != t:
+            _refuse(name, f"x must be a matrix of {t} rows on the current device, not {tuple(size)}")
+        width = size[1]
+        x_stride, unit = x.stride()
+        if unit != 1 and width > 1:
+            _refuse_matrix(name, "x", x)
+        dtype = DTYPES.get(x.dtype)
+        if dtype is None:
+            _refuse_type(name, "x", x)
         if rows is None:
-            rows, rows_stride = x.new_empty((slots, width)), width
-        else:
-            rows_stride = _matrix_like(name, "rows", rows, device, (slots, width), x.dtype, True)
+            rows = x.new_empty((slots, width))
+        elif rows.dtype is not x.dtype or rows.shape != (slots, width) or rows.get_device() != device:
+            _refuse_like(name, "rows", rows, (slots, width), x.dtype)
+        rows_stride, unit = rows.stride()
+        if (unit != 1 and width > 1) or (rows_stride < width and slots > 1):
+            _refuse_like(name, "rows", rows, (slots, width), x.dtype)
+        if slots <= 1:
+            rows_stride = width
         x_ptr, rows_ptr = x.data_ptr(), rows.data_ptr()
     elif rows is not None:
         _refuse(name, "rows without x")
@@ -218,24 +226,35 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
 
 
 def _combine(name, rows, pos, weights, out, stream):
-    device = _first(name, "rows", rows)
-    n, width, stride = _matrix(name, "rows", rows, device)
-    shape = pos.shape
-    if len(shape) != 2:
-        _refuse(name, "pos must have two dimensions")
+    device, size, shape = rows.get_device(), rows.shape, pos.shape
+    if device < 0 or device != _device() or len(size) != 2:
+        _refuse_matrix(name, "rows", rows)
+    n, width = size
+    stride, unit = rows.stride()
+    if unit != 1 and width > 1:
+        _refuse_matrix(name, "rows", rows)
+    dtype = DTYPES.get(rows.dtype)
+    if dtype is None:
+        _refuse_type(name, "rows", rows)
+    if pos.dtype is not _I32 or len(shape) != 2 or pos.get_device() != device or not pos.is_contiguous():
+        _refuse(name, f"pos must be a contiguous int32 matrix on the current device, not {pos.dtype} {tuple(shape)}")
     t, k = shape
-    _dense(name, "pos", pos, device, shape, torch.int32)
     w_ptr = None
     if weights is not None:
-        _dense(name, "weights", weights, device, shape, torch.float32)
+        if weights.dtype is not _F32 or weights.shape != shape or weights.get_device() != device or not weights.is_contiguous():
+            _refuse_dense(name, "weights", weights, shape, _F32)
         w_ptr = weights.data_ptr()
-    handle = _stream(name, stream, device, out is not None)
+    handle = _raw_stream(device) if stream is None else _stream(name, stream, device, out is not None)
     if out is None:
-        out, out_stride = rows.new_empty((t, width)), width
-    else:
-        out_stride = _matrix_like(name, "out", out, device, (t, width), rows.dtype, True)
+        out = rows.new_empty((t, width))
+    elif out.dtype is not rows.dtype or out.shape != (t, width) or out.get_device() != device:
+        _refuse_like(name, "out", out, (t, width), rows.dtype)
+    out_stride, unit = out.stride()
+    if (unit != 1 and width > 1) or (out_stride < width and t > 1):
+        _refuse_like(name, "out", out, (t, width), rows.dtype)
     status = (bfs._lib or bfs.lib()).bfs_moe_combine(
-        rows.data_ptr(), _dtype(name, rows), n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(), out_stride, handle)
+        rows.data_ptr(), dtype, n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(), out_stride if t > 1 else width,
+        handle)
     if status:
         bfs._check(status)
     return out
@@ -260,26 +279,45 @@ def moe_combine_grad(grad_y, rows, pos, weights, *, grad_rows=None, grad_weights
     rows[pos[t, j]]>.  Rows that no slot names are left as they were (zeros in
     a grad_rows that the call allocates)."""
     name = "moe_combine_grad"
-    device = _first(name, "grad_y", grad_y)
-    t, width, dy_stride = _matrix(name, "grad_y", grad_y, device)
-    n = rows.shape[0]
-    rows_stride = _matrix_like(name, "rows", rows, device, (n, width), grad_y.dtype)
+    device, size, shape = grad_y.get_device(), grad_y.shape, rows.shape
+    if device < 0 or device != _device() or len(size) != 2:
+        _refuse_matrix(name, "grad_y", grad_y)
+    t, width = size
+    dy_stride, unit = grad_y.stride()
+    if unit != 1 and width > 1:
+        _refuse_matrix(name, "grad_y", grad_y)
+    dtype = DTYPES.get(grad_y.dtype)
+    if dtype is None:
+        _refuse_type(name, "grad_y", grad_y)
+    if rows.dtype is not grad_y.dtype or len(shape) != 2 or shape[1] != width or rows.get_device() != device:
+        _refuse(name, f"rows must be {grad_y.dtype} of {width} columns on the current device, not {rows.dtype} {tuple(shape)}")
+    n = shape[0]
+    rows_stride, unit = rows.stride()
+    if unit != 1 and width > 1:
+        _refuse_matrix(name, "rows", rows)
     k = pos.shape[-1]
-    shape = (t, k)
-    _dense(name, "pos", pos, device, shape, torch.int32)
-    _dense(name, "weights", weights, device, shape, torch.float32)
-    handle = _stream(name, stream, device, grad_rows is not None and grad_weights is not None)
+    slots = (t, k)
+    if pos.dtype is not _I32 or pos.shape != slots or pos.get_device() != device or not pos.is_contiguous():
+        _refuse_dense(name, "pos", pos, slots, _I32)
+    if weights.dtype is not _F32 or weights.shape != slots or weights.get_device() != device or not weights.is_contiguous():
+        _refuse_dense(name, "weights", weights, slots, _F32)
+    handle = _raw_stream(device) if stream is None else _stream(name, stream, device,
+                                                                grad_rows is not None and grad_weights is not None)
     if grad_rows is None:
-        grad_rows, out_stride = rows.new_zeros((n, width)), width
-    else:
-        out_stride = _matrix_like(name, "grad_rows", grad_rows, device, (n, width), grad_y.dtype, True)
+        grad_rows = rows.new_zeros(shape)
+    elif grad_rows.dtype is not grad_y.dtype or grad_rows.shape != shape or grad_rows.get_device() != device:
+        _refuse_like(name, "grad_rows", grad_rows, shape, grad_y.dtype)
+    out_stride, unit = grad_rows.stride()
+    if (unit != 1 and width > 1) or (out_stride < width and n > 1):
+        _refuse_like(name, "grad_rows", grad_rows, shape, grad_y.dtype)
     if grad_weights is None:
-        grad_weights = weights.new_empty(shape)
-    else:
-        _dense(name, "grad_weights", grad_weights, device, shape, torch.float32)
+        grad_weights = weights.new_empty(slots)
+    elif (grad_weights.dtype is not _F32 or grad_weights.shape != slots or grad_weights.get_device() != device
+          or not grad_weights.is_contiguous()):
+        _refuse_dense(name, "grad_weights", grad_weights, slots, _F32)
     status = (bfs._lib or bfs.lib()).bfs_moe_combine_grad(
-        grad_y.data_ptr(), _dtype(name, grad_y), t, width, dy_stride, rows.data_ptr(), n, rows_stride, pos.data_ptr(),
-        weights.data_ptr(), k, grad_rows.data_ptr(), out_stride, grad_weights.data_ptr(), handle)
+        grad_y.data_ptr(), dtype, t, width, dy_stride, rows.data_ptr(), n, rows_stride, pos.data_ptr(), weights.data_ptr(), k,
+        grad_rows.data_ptr(), out_stride if n > 1 else width, grad_weights.data_ptr(), handle)
     if status:
         bfs._check(status)
     return grad_rows, grad_weights
@@ -302,7 +340,9 @@ class GradSet:
         for g in grads:
             if not isinstance(g, torch.Tensor) or not g.is_cuda or not g.is_contiguous():
                 _refuse(name, "gradients must be contiguous tensors on a device")
-        types = [_dtype(name, g) for g in grads]
+            if g.dtype not in DTYPES:
+                _refuse_type(name, "a gradient", g)
+        types = [DTYPES[g.dtype] for g in grads]
         sizes = [g.numel() for g in grads]
         if out is None:
             outs = grads
@@ -343,14 +383,15 @@ class GradSet:
         self.workspace_bytes = self._set.workspace_bytes
 
     def _buffers(self, name, norm, workspace, stream):
-        device = _device()
-        if device != self._device and self._device is not None:
+        device = _device() if self._device is None else self._device
+        if device != _device():
             _refuse(name, "the gradients are not on the current device")
-        handle = _stream(name, stream, device, norm is not None and workspace is not None)
+        handle = _raw_stream(device) if stream is None else _stream(name, stream, device,
+                                                                    norm is not None and workspace is not None)
         if norm is None:
-            norm = torch.empty((), dtype=torch.float32, device="cuda")
-        else:
-            _dense(name, "norm", norm, device, (), torch.float32)
+            norm = torch.empty((), dtype=_F32, device="cuda")
+        elif norm.dtype is not _F32 or norm.dim() != 0 or norm.get_device() != device:
+            _refuse_dense(name, "norm", norm, (), _F32)
         if workspace is None:
             return norm, norm.new_empty(self.workspace_bytes, dtype=torch.uint8), self.workspace_bytes, handle
         if workspace.get_device() != device or not workspace.is_contiguous():
