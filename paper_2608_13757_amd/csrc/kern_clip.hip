@@ -47,14 +47,14 @@ struct Entry {
   int64_t n;
   int32_t first, chunks;
   int32_t type;                  // bfs_dtype of in | of out << 4
-  int32_t pad;
+  int32_t index;                 // in the table
 };
 
-// The table in device memory: the entries, then the entry that holds each
-// workgroup's first chunk.
+// The table in device memory: the entries, then for each workgroup a copy of
+// the entry that holds its first chunk (one access instead of two in a row).
 struct Table {
   const Entry *entry;
-  const int32_t *start;
+  const Entry *start;
   int64_t chunk;
   int32_t n_chunks;
 };
@@ -134,10 +134,9 @@ __device__ __forceinline__ double square_sum(const Entry &e, int64_t chunk, int 
 __global__ void __launch_bounds__(kThreads) square_kernel(Table t, double *partial) {
   const int from = first_chunk(t, (int)blockIdx.x), to = first_chunk(t, (int)blockIdx.x + 1);
   double s = 0.0;
-  int i = t.start[blockIdx.x];
+  Entry e = t.start[blockIdx.x];
   for (int c = from; c < to; ++c) {
-    while (t.entry[i].first + t.entry[i].chunks <= c) ++i;
-    const Entry e = t.entry[i];
+    if (e.first + e.chunks <= c) e = t.entry[e.index + 1];
     switch (e.type & 15) {
       case BFS_DTYPE_F32: s += square_sum<float>(e, t.chunk, c - e.first); break;
       case BFS_DTYPE_BF16: s += square_sum<__bf16>(e, t.chunk, c - e.first); break;
@@ -183,17 +182,16 @@ __device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c
 }
 
 __global__ void __launch_bounds__(kThreads) clip_kernel(Table t, const double *partial, double max_norm, float *norm) {
+  const int back = (int)(gridDim.x - 1 - blockIdx.x);
+  Entry e = t.start[back];                         // on its way under the sums
   const double root = sqrt(total_of(partial, (int)gridDim.x));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
   const double ratio = max_norm / (root + kEps);
   const float scale = isfinite(root) && ratio < 1.0 ? (float)ratio : 1.0f;
-  const int back = (int)(gridDim.x - 1 - blockIdx.x);
   const int from = first_chunk(t, back), to = first_chunk(t, back + 1);
-  int i = t.start[back];
-  while (t.entry[i].first + t.entry[i].chunks < to) ++i;
+  while (e.first + e.chunks < to) e = t.entry[e.index + 1];
   for (int c = to - 1; c >= from; --c) {
-    while (t.entry[i].first > c) --i;
-    const Entry e = t.entry[i];
+    if (e.first > c) e = t.entry[e.index - 1];
     if (scale == 1.0f && e.in == e.out) continue;
     switch (e.type) {
       case BFS_DTYPE_F32: scale_chunk<float, float>(e, t.chunk, c - e.first, scale); break;
@@ -210,7 +208,7 @@ int64_t chunks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
 Table table_of(const bfs_grad_set &set, const void *image) {
   Table t;
   t.entry = static_cast<const Entry *>(image);
-  t.start = reinterpret_cast<const int32_t *>(t.entry + set.n_entries);
+  t.start = t.entry + set.n_entries;
   t.chunk = set.chunk;
   t.n_chunks = set.n_chunks;
   return t;
@@ -263,7 +261,7 @@ bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int
     s.n_chunks = (int32_t)chunks;
     s.n_blocks = chunks < kBlocks ? (int32_t)chunks : kBlocks;
     s.workspace_bytes = (s.n_blocks > 0 ? s.n_blocks : 1) * (int64_t)sizeof(double);
-    s.image_bytes = held * (int64_t)sizeof(Entry) + s.n_blocks * (int64_t)sizeof(int32_t);
+    s.image_bytes = ((int64_t)held + s.n_blocks) * (int64_t)sizeof(Entry);
     if (image) {
       if (image_bytes < s.image_bytes) return fail(BFS_E_INVALID, "grad_table: image of " + std::to_string(s.image_bytes) + " bytes needed");
       unsigned char *p = static_cast<unsigned char *>(image);
@@ -278,12 +276,12 @@ bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int
         e.first = (int32_t)first;
         e.chunks = (int32_t)chunks_of(numel[i], s.chunk);
         e.type = dtypes[i] | out_dtypes[i] << 4;
+        e.index = k;
         first += e.chunks;
+        std::memcpy(p + k++ * sizeof(Entry), &e, sizeof e);
         // workgroups that begin in this tensor
         for (; b < s.n_blocks && chunks * b / s.n_blocks < first; ++b)
-          std::memcpy(p + held * sizeof(Entry) + b * sizeof(int32_t), &k, sizeof k);
-        std::memcpy(p + k * sizeof(Entry), &e, sizeof e);
-        ++k;
+          std::memcpy(p + ((int64_t)held + b) * sizeof(Entry), &e, sizeof e);
       }
     }
     *set = s;

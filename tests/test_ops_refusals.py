@@ -2,6 +2,7 @@
 returns an error (or has nothing to do) before anything would be launched, so
 the addresses are never used."""
 import ctypes as C
+import struct
 import subprocess
 import sys
 
@@ -140,11 +141,11 @@ def test_workspaces():
 
 
 def _entries(made, buf):
-    """(in, out, n, first, chunks, type) of each tensor, and each workgroup's first one."""
-    import struct
+    """(in, out, n, first, chunks, type, index) of each tensor, and of the one that each workgroup begins in."""
     raw = buf.raw[:made.image_bytes]
-    rows = [struct.unpack_from("<QQqiiii", raw, 40 * i)[:6] for i in range(made.n_entries)]
-    return rows, struct.unpack_from("<%di" % made.n_blocks, raw, 40 * made.n_entries)
+    assert len(raw) == 40 * (made.n_entries + made.n_blocks)
+    rows = [struct.unpack_from("<QQqiiii", raw, 40 * i) for i in range(made.n_entries + made.n_blocks)]
+    return rows[:made.n_entries], rows[made.n_entries:]
 
 
 @pytest.mark.parametrize("sizes", [[1], [5, 0, 100000, 3, 0, 16384], [1] * 2000, [7] + [1 << 20] * 30, [1 << 33, 9], []])
@@ -157,13 +158,14 @@ def test_grad_table(sizes):
     rows, start = _entries(made, buf)
     assert [r[2] for r in rows] == [s for s in sizes if s] and all(r[0] == r[1] == A and r[5] == BF16 * 17 for r in rows)
     at = 0
-    for _, _, size, first, chunks, _ in rows:
+    assert [r[6] for r in rows] == list(range(len(rows)))
+    for _, _, size, first, chunks, _, _ in rows:
         assert first == at and (chunks - 1) * made.chunk < size <= chunks * made.chunk
         at += chunks
     assert at == made.n_chunks and made.n_blocks == min(at, 1024) == len(start)
-    for b, i in enumerate(start):
+    for b, r in enumerate(start):
         c = made.n_chunks * b // made.n_blocks
-        assert rows[i][3] <= c < rows[i][3] + rows[i][4]
+        assert r == rows[r[6]] and r[3] <= c < r[3] + r[4]
 
 
 def test_package_imports_without_the_operators():
