@@ -385,7 +385,7 @@ bfs_status bfs_run_status(const bfs_plan *plan, struct ihipStream_t *stream);
  * in elements: an output's at least the width, an input's anything from 0
  * (one row for all).  Rows need no more than their element's alignment.
  * Outputs must not overlap inputs or each other except where it is said.
- * At most 2^24 - 1 tokens.
+ * At most 2^24 - 1 tokens and 2^28 columns.
  */
 typedef enum { BFS_DTYPE_F32 = 0, BFS_DTYPE_BF16 = 1, BFS_DTYPE_F16 = 2 } bfs_dtype;
 
@@ -461,7 +461,9 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
  * once for n_tensors contiguous tensors (host arrays: addresses, numel[i]
  * elements of dtypes[i]) and their outputs: each has its gradient's type, and
  * may then be the gradient itself, or is fp32 (a part of the AdamW family's
- * flat gradient, say).  bfs_grad_table fills *set and, where image is given,
+ * flat gradient, say).  Gradients may share memory; an output shares none with
+ * another output or another gradient, or bfs_grad_clip refuses the set
+ * (bfs_grad_norm does not read the outputs).  bfs_grad_table fills *set and, where image is given,
  * writes the table of set->image_bytes bytes to it (host memory; call once
  * with NULL for the size).  The caller lays the table into device memory
  * (aligned to 16 bytes), which, like the tensors, must stay as it is while
@@ -472,7 +474,8 @@ typedef struct {
   int64_t image_bytes;           /* device memory of the table */
   int64_t workspace_bytes;       /* device memory that a call works in */
   int64_t chunk;                 /* the launches' shape, the library's own */
-  int32_t n_entries, n_chunks, n_blocks, reserved;
+  int32_t n_entries, n_chunks, n_blocks;
+  int32_t overlap;               /* not 0: outputs overlap, bfs_grad_clip refuses */
 } bfs_grad_set;
 
 bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
@@ -489,7 +492,7 @@ bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *
 
 /*
  * outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6)).  Where the norm is
- * not finite the scale is 1.  norm: NULL, or where the norm (before clipping)
+ * not finite (in fp32) the scale is 1.  norm: NULL, or where the norm (before clipping)
  * goes.  max_norm >= 0.
  */
 bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double max_norm, float *norm, void *workspace,

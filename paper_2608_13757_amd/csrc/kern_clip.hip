@@ -7,7 +7,7 @@
 // fp32's range from 2^64 on, and the sum is as long as the model), each
 // workgroup over its own chunks in their order, the workgroups' sums in the
 // order of the workgroups: the same bits in every run.  A norm that is not
-// finite leaves in-place gradients as they are and copies them (cast) to a
+// finite (in fp32, as it is reported) leaves in-place gradients as they are and copies them (cast) to a
 // separate output, so that the caller sees them next to the norm that says so.
 //
 // Two passes over the gradients, since the scale depends on all of them;
@@ -20,8 +20,10 @@
 //
 // 2^28 bf16 gradients in 290 tensors into fp32: 405 us, 5.3 TB/s over both
 // passes, a large copy's rate; 2^20 fp32 in 24: 9 us, two short launches.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <vector>
 
 #include "op_common.h"
 
@@ -158,13 +160,24 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const double *partial, i
   if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
+struct Scale {
+  float first, then;             // g * first is exact wherever the result is not 0
+};
+
+// Below 2^-100 a factor of 2^-63 is taken out first: the rest stays a normal
+// number (huge gradients and a small max_norm), and what that factor makes
+// subnormal would round to 0 in the end.
+__device__ __forceinline__ Scale scale_of(double ratio) {
+  return ratio < 0x1p-100 ? Scale{0x1p-63f, (float)(ratio * 0x1p63)} : Scale{1.0f, (float)ratio};
+}
+
 // A lane's access is 16 bytes of the output, where the chunks begin with a
 // line: into a flat vector, in which tensors begin anywhere, whole lines are
 // written.  Nontemporal stores leave the last-level cache to the gradients that
 // the pass is still to read (2^25 fp32: 64 us with plain stores, 45 with these;
 // 2^23 and below: the same).
 template <typename T, typename U>
-__device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c, float scale) {
+__device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c, Scale s) {
   constexpr int V = Chunk<U>::kElems;
   typedef T in_vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));
   typedef typename Chunk<U>::vec vec;
@@ -175,10 +188,10 @@ __device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c
       [&](int64_t i, in_vec v) {
         vec o;
 #pragma unroll
-        for (int j = 0; j < V; ++j) o[j] = (U)((float)v[j] * scale);
+        for (int j = 0; j < V; ++j) o[j] = (U)((float)v[j] * s.first * s.then);
         __builtin_nontemporal_store(o, reinterpret_cast<vec *>(out + i));
       },
-      [&](int64_t i) { out[i] = (U)((float)g[i] * scale); });
+      [&](int64_t i) { out[i] = (U)((float)g[i] * s.first * s.then); });
 }
 
 __global__ void __launch_bounds__(kThreads) clip_kernel(Table t, const double *partial, double max_norm, float *norm) {
@@ -187,12 +200,13 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(Table t, const double *p
   const double root = sqrt(total_of(partial, (int)gridDim.x));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
   const double ratio = max_norm / (root + kEps);
-  const float scale = isfinite(root) && ratio < 1.0 ? (float)ratio : 1.0f;
+  const bool clips = isfinite((float)root) && ratio < 1.0;
+  const Scale scale = scale_of(clips ? ratio : 1.0);
   const int from = first_chunk(t, back), to = first_chunk(t, back + 1);
   while (e.first + e.chunks < to) e = t.entry[e.index + 1];
   for (int c = to - 1; c >= from; --c) {
     if (e.first > c) e = t.entry[e.index - 1];
-    if (scale == 1.0f && e.in == e.out) continue;
+    if (!clips && e.in == e.out) continue;
     switch (e.type) {
       case BFS_DTYPE_F32: scale_chunk<float, float>(e, t.chunk, c - e.first, scale); break;
       case BFS_DTYPE_BF16: scale_chunk<__bf16, float>(e, t.chunk, c - e.first, scale); break;
@@ -201,6 +215,35 @@ __global__ void __launch_bounds__(kThreads) clip_kernel(Table t, const double *p
       default: scale_chunk<_Float16, _Float16>(e, t.chunk, c - e.first, scale); break;
     }
   }
+}
+
+// Whether an output shares memory with another one, or with a gradient that is
+// not its own (or its own, elsewhere): no order of the writes is right then.
+bool overlaps(const void *const *grads, void *const *outs, const int64_t *numel, const int32_t *dtypes,
+              const int32_t *out_dtypes, int32_t n) {
+  struct Span {
+    uintptr_t from, to;
+    int32_t i;
+  };
+  auto span = [&](const void *p, int32_t i, int32_t dtype) {
+    const uintptr_t from = (uintptr_t)p;
+    return Span{from, from + (uintptr_t)numel[i] * (dtype == BFS_DTYPE_F32 ? 4 : 2), i};
+  };
+  std::vector<Span> out;
+  for (int32_t i = 0; i < n; ++i)
+    if (numel[i] > 0) out.push_back(span(outs[i], i, out_dtypes[i]));
+  std::sort(out.begin(), out.end(), [](const Span &a, const Span &b) { return a.from < b.from; });
+  for (size_t i = 1; i < out.size(); ++i)
+    if (out[i].from < out[i - 1].to) return true;
+  for (int32_t i = 0; i < n; ++i) {
+    if (numel[i] == 0) continue;
+    const Span g = span(grads[i], i, dtypes[i]);
+    // the outputs are apart, so ends ascend too: from the first that ends behind g's start
+    auto o = std::upper_bound(out.begin(), out.end(), g.from, [](uintptr_t a, const Span &b) { return a < b.to; });
+    for (; o != out.end() && o->from < g.to; ++o)
+      if (o->i != i || o->from != g.from) return true;
+  }
+  return false;
 }
 
 int64_t chunks_of(int64_t n, int64_t chunk) { return (n + chunk - 1) / chunk; }
@@ -261,6 +304,7 @@ bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int
     s.n_chunks = (int32_t)chunks;
     s.n_blocks = chunks < kBlocks ? (int32_t)chunks : kBlocks;
     s.workspace_bytes = (s.n_blocks > 0 ? s.n_blocks : 1) * (int64_t)sizeof(double);
+    s.overlap = overlaps(grads, outs, numel, dtypes, out_dtypes, n_tensors);
     s.image_bytes = ((int64_t)held + s.n_blocks) * (int64_t)sizeof(Entry);
     if (image) {
       if (image_bytes < s.image_bytes) return fail(BFS_E_INVALID, "grad_table: image of " + std::to_string(s.image_bytes) + " bytes needed");
@@ -308,6 +352,8 @@ bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double 
   return entry([&]() -> bfs_status {
     bfs_status st = check_call("grad_clip", set, dev_image, workspace, workspace_bytes);
     if (st == BFS_OK && !(max_norm >= 0.0)) st = fail(BFS_E_INVALID, "grad_clip: max_norm must not be negative");
+    if (st == BFS_OK && set->overlap)
+      st = fail(BFS_E_INVALID, "grad_clip: an output overlaps another one or a gradient that is not its own");
     if (st != BFS_OK) return st;
     double *partial = static_cast<double *>(workspace);
     if (set->n_blocks == 0) return norm ? launch("grad_clip", norm_kernel, 1, kThreads, 0, stream, partial, 0, norm) : BFS_OK;

@@ -222,8 +222,8 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(CombineParams P)
 bfs_status check_rows(const char *what, int64_t n_rows, int64_t width, int64_t n_tokens, int32_t k) {
   if (n_rows < 0 || width < 0 || n_tokens < 0 || k < 1)
     return fail(BFS_E_INVALID, std::string(what) + ": a negative or zero size");
-  if (k > kMaxK || n_tokens > kMaxTokens || n_rows >= (int64_t)1 << 31)
-    return fail(BFS_E_RESOURCE, std::string(what) + ": at most 64 experts per token, 2^24 - 1 tokens and 2^31 - 1 rows");
+  if (k > kMaxK || n_tokens > kMaxTokens || n_rows >= (int64_t)1 << 31 || width > kMaxWidth)
+    return fail(BFS_E_RESOURCE, std::string(what) + ": at most 64 experts per token, 2^24 - 1 tokens, 2^31 - 1 rows and 2^28 columns");
   return BFS_OK;
 }
 

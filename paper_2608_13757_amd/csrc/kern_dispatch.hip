@@ -127,11 +127,11 @@ __device__ __forceinline__ void rank_slots(const DispatchParams &P, const int (&
       const uint32_t before = __hip_atomic_load(h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
       const int rank = __popcll(same & below);
       row[b] = (int)(base[id[b]] + before) + rank;
-      __builtin_amdgcn_wave_barrier();
+      wave_sync();
       if (rank == 0)
         __hip_atomic_store(h, before + (uint32_t)__popcll(same), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_sync();
   }
 }
 
@@ -319,6 +319,7 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       return fail(BFS_E_INVALID, "moe_dispatch: x and rows are given together");
     if (x && (width < 0 || x_stride < 0 || rows_stride < width))
       return fail(BFS_E_INVALID, "moe_dispatch: negative stride or width, or rows that overlap");
+    if (x && width > kMaxWidth) return fail(BFS_E_RESOURCE, "moe_dispatch: at most 2^28 columns");
     if (need > 0 && (!workspace || workspace_bytes < need))
       return fail(BFS_E_INVALID, "moe_dispatch: workspace of " + std::to_string(need) + " bytes needed");
     if ((uintptr_t)workspace % sizeof(uint32_t)) return fail(BFS_E_INVALID, "moe_dispatch: workspace not aligned to 4 bytes");

@@ -159,7 +159,7 @@ __device__ __forceinline__ void select(uint32_t (&key)[N], int l, int k, uint32_
       }
       if (has) mine[j] = make_uint2(m, e);
     }
-    __builtin_amdgcn_wave_barrier();                               // a wave's LDS accesses complete in order
+    wave_sync();
     if (l < k) {
       const uint2 f = mine[l];
       my_key = f.x;
@@ -278,9 +278,9 @@ __global__ void __launch_bounds__(kThreads) route_grad_kernel(const T *logits, i
     term = g;
   }
   term = sum_equal<G>(e, term, k);
-  __builtin_amdgcn_wave_barrier();                                 // a wave's LDS accesses complete in order
+  wave_sync();
   if (e >= 0) terms[e] = term;
-  __builtin_amdgcn_wave_barrier();
+  wave_sync();
   if (!live) return;
   T *out = grad_logits + token * grad_stride;
   typedef T vec __attribute__((ext_vector_type(V), aligned(sizeof(T))));

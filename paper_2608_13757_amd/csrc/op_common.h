@@ -16,7 +16,8 @@ namespace bfsop {
 using bfs::fail;
 
 constexpr int kWave = 64;
-constexpr int64_t kMaxTokens = ((int64_t)1 << 24) - 1;
+// With these and at most 64 slots a token, byte counts stay below 2^63.
+constexpr int64_t kMaxTokens = ((int64_t)1 << 24) - 1, kMaxWidth = (int64_t)1 << 28;
 
 // 16 bytes of a row.  Rows start at any element (odd widths, views), so the
 // alignment is the element's; global accesses of four words need no more.
@@ -148,6 +149,16 @@ __device__ __forceinline__ float group_sum(float x) {
 // Wave index in the workgroup, in a scalar register.
 __device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
 __device__ __forceinline__ int lane_index() { return (int)(threadIdx.x & 63u); }
+
+// Between LDS accesses of a wave's lanes to each other's words.  The hardware
+// completes a wave's LDS accesses in order; the fences, which cost no
+// instruction at this scope, keep the compiler from taking a value that this
+// lane stored for one that another lane may have stored since.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 template <typename... P, typename... A>
 bfs_status launch(const char *what, void (*kernel)(P...), int64_t blocks, int threads, size_t lds, void *stream, A... a) {

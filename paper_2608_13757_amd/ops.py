@@ -4,7 +4,8 @@ norm with clipping.
 
 Argument checks and marshalling only.  Tensors are torch tensors on the
 current device; a refused argument raises BfsError (E_INVALID or E_RESOURCE)
-before anything is launched.  Outputs that are not given are allocated on the
+before anything is launched.  An output must not share memory with an input or
+another output, except where it is said.  Outputs that are not given are allocated on the
 current stream.  ``stream``: a torch stream or handle, None the current one;
 on another stream than the current one every output (and the workspace) has to
 be given, since an allocation belongs to the stream that it was made on.
@@ -21,10 +22,11 @@ import struct
 import torch
 
 from . import bfs
-from .bfs import E_INVALID, OK, BfsError
+from .bfs import E_INVALID, E_RESOURCE, OK, BfsError
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOE_RENORMALIZE = 1
+MAX_EXPERTS = 1024
 DISPATCH_ONE_GROUP = 1024        # slots of one group: at most one needs no workspace
 _I32, _F32 = torch.int32, torch.float32
 
@@ -57,9 +59,15 @@ def _refuse_type(name, what, t):
     _refuse(name, f"{what} of type {t.dtype} (float32, bfloat16 and float16 are supported)")
 
 
+def _refuse_experts(name, n_experts):
+    raise BfsError(E_INVALID if n_experts < 1 else E_RESOURCE, f"{name}: n_experts = {n_experts} (1 .. {MAX_EXPERTS})")
+
+
 def _stream(name, stream, device, given):
     """Handle of a stream; ``given``: whether nothing has to be allocated."""
     handle = bfs._stream_handle(stream)
+    if getattr(stream, "device_index", device) != device:
+        _refuse(name, "the stream belongs to another device")
     if not given and handle != _raw_stream(device):
         _refuse(name, "on another stream than the current one every output and the workspace must be given")
     return handle
@@ -88,8 +96,8 @@ def moe_route(logits, k, *, renormalize=True, experts=None, weights=None, stream
     dtype = DTYPES.get(logits.dtype)
     if dtype is None:
         _refuse_type(name, "logits", logits)
-    if k < 1:
-        _refuse(name, f"k = {k}")
+    if not 1 <= k <= e:
+        _refuse(name, f"k = {k} of {e} experts")
     handle = _raw_stream(device) if stream is None else _stream(name, stream, device, experts is not None and weights is not None)
     shape = (t, k)
     if experts is None:
@@ -147,6 +155,8 @@ def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logi
 
 def moe_dispatch_workspace(n_tokens, k, n_experts):
     """Bytes of device memory that a dispatch of these sizes works in."""
+    if n_experts > MAX_EXPERTS:
+        _refuse_experts("moe_dispatch_workspace", n_experts)
     n = C.c_int64()
     _call(bfs.lib().bfs_moe_dispatch_workspace, n_tokens, k, n_experts, C.byref(n))
     return n.value
@@ -165,8 +175,8 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
     device, shape = experts.get_device(), experts.shape
     if device < 0 or device != _device() or len(shape) != 2 or experts.dtype is not _I32 or not experts.is_contiguous():
         _refuse(name, f"experts must be a contiguous int32 matrix on the current device, not {experts.dtype} {tuple(shape)}")
-    if n_experts < 1:
-        _refuse(name, f"n_experts = {n_experts}")
+    if not 1 <= n_experts <= MAX_EXPERTS:
+        _refuse_experts(name, n_experts)
     t, k = shape
     slots = t * k
     one_group = k and slots <= DISPATCH_ONE_GROUP // k * k
@@ -331,7 +341,9 @@ class GradSet:
     other (float32, or the type of all of them: the gradient buffer of an
     AdamW plan), or a tensor for each.  Like a plan its program, the set keeps
     a table of the tensors on the device, and their memory: a gradient that is
-    allocated anew needs a new set.  Making one copies the table (it waits for
+    allocated anew needs a new set.  A gradient named twice counts twice in the
+    norm; a set whose outputs overlap (that one in place, say) is not clipped.
+    Making one copies the table (it waits for
     the copy and cannot be captured); the calls can be."""
 
     def __init__(self, grads, out=None):
@@ -406,8 +418,8 @@ class GradSet:
 
     def clip(self, max_norm, norm=None, workspace=None, stream=None):
         """Writes grads * min(1, max_norm / (norm + 1e-6)) to the outputs and
-        returns the norm before clipping.  A norm that is not finite scales by
-        1."""
+        returns the norm before clipping.  A norm that is not finite (in
+        float32) scales by 1."""
         norm, workspace, size, handle = self._buffers("grad_clip", norm, workspace, stream)
         _call(bfs._lib.bfs_grad_clip, *self._args, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle)
         return norm

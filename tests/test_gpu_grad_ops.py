@@ -129,6 +129,48 @@ def test_shared_gradient_counts_twice_in_the_norm():
     assert abs(float(GradSet([g, g]).norm()) - 2 ** 0.5 * _norm64([g])) <= 4 * U * _norm64([g])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("max_norm", [1e-3, 1e-12])
+def test_scale_below_fp32(dtype, max_norm):
+    """Norms near fp32's largest value: the scale is below its normal numbers,
+    the clipped gradients are not (two roundings of scale and product, as
+    ever, and the norm's)."""
+    g = torch.Generator().manual_seed(8)
+    grads = [(torch.rand(1000, generator=g) * 2e38 / 40).to(dtype).cuda(), torch.tensor([1.0, -2e-30, 0.0], dtype=dtype).cuda()]
+    ref = _check_norm(GradSet(grads).norm(), grads)
+    out = torch.empty(1003, device="cuda")
+    GradSet(grads, out=out).clip(max_norm)
+    for o, x in zip(out.split([1000, 3]), grads):
+        _check_out(o, x, max_norm / (ref + 1e-6), torch.float32)
+    assert abs(_norm64([out]) - max_norm) <= 1e-5 * max_norm
+
+
+def test_norm_beyond_fp32():
+    """A norm that fp32 does not hold is reported as infinite, and nothing is
+    scaled, as the documentation says."""
+    g = torch.full((5000,), 3e38, device="cuda")
+    out = torch.empty_like(g)
+    assert GradSet([g], out=out).clip(1.0) == float("inf") and torch.equal(out, g)
+
+
+def test_overlapping_outputs():
+    """Refused by the clipping; their norm is as good as any."""
+    buf = _grads(9, [1000], [torch.float32])[0]
+    a, b, c = buf[:400], buf[400:], buf[300:500]
+    for grads, out in (([a, a], None), ([a, c], None), ([a, b], [buf[100:500], b.clone()])):
+        s, before = GradSet(grads, out=out), buf.clone()
+        _check_norm(s.norm(), grads)
+        with pytest.raises(BfsError) as e:
+            s.clip(0.1)
+        assert e.value.status == bfs.E_INVALID and torch.equal(buf, before)
+    # gradients that share memory, to outputs of their own; neighbours in place
+    for grads, out in (([a, c], [torch.empty_like(a), torch.empty_like(c)]), ([a, b], None), ([a, b], buf)):
+        want = torch.cat(grads).double() * min(1.0, 0.1 / (_norm64(grads) + 1e-6))
+        GradSet(grads, out=out).clip(0.1)
+        got = torch.cat(out if isinstance(out, list) else [a, b]).double()
+        assert (got - want).abs().max() <= 4 * U * want.abs().max()
+
+
 def test_refusals():
     g = torch.zeros(8, device="cuda")
     for call in (lambda: GradSet([g.cpu()]), lambda: GradSet([g[::2]]), lambda: GradSet([g.int()]),

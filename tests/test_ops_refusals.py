@@ -91,6 +91,7 @@ INVALID = [
     (_table, dict(made=False)), (_grad_call, dict(set_=False)), (_grad_call, dict(image=None)), (_grad_call, dict(image=A + 8)),
     (_grad_call, dict(norm=None)), (_grad_call, dict(ws=None)), (_grad_call, dict(ws_bytes=4)), (_grad_call, dict(ws=A + 4)),
     (_grad_call, dict(max_norm=-1.0)), (_grad_call, dict(max_norm=float("nan"))), (_grad_call, dict(max_norm=1.0, ws=None)),
+    (_grad_call, dict(max_norm=1.0, change=("overlap", 1))),
     (_grad_call, dict(change=("n_blocks", 0))), (_grad_call, dict(change=("n_blocks", 1 << 20))),
     (_grad_call, dict(change=("chunk", 0))), (_grad_call, dict(change=("n_entries", -1))),
 ]
@@ -105,6 +106,8 @@ def test_invalid_arguments(call, kw):
 RESOURCE = [(_route, dict(e=1025, stride=1025)), (_route, dict(e=64, stride=64, k=17)), (_route, dict(t=1 << 31)),
             (_dispatch, dict(e=1025)), (_dispatch, dict(k=65)), (_dispatch, dict(t=1 << 30)), (_combine, dict(k=65)),
             (_combine, dict(t=1 << 30)), (_combine, dict(n=1 << 31)), (_combine_grad, dict(t=1 << 30)),
+            (_dispatch, dict(width=1 << 62, x_stride=1 << 62, rows_stride=1 << 62)), (_combine, dict(width=(1 << 28) + 1, y_stride=1 << 30)),
+            (_combine_grad, dict(width=1 << 40, out_stride=1 << 40)),
             (_table, dict(numel=(1 << 44,))),
             (_table, dict(grads=(A, A), outs=(A, A), numel=(1 << 42, 1 << 43), dtypes=(F32, F32), out_dtypes=(F32, F32)))]
 
@@ -136,6 +139,10 @@ def test_workspaces():
         with pytest.raises(BfsError) as e:
             moe_dispatch_workspace(*bad)
         assert e.value.status == bfs.E_INVALID
+    for n_experts in (1025, (1 << 32) + 8):           # (no 32 bits of it pass for another number)
+        with pytest.raises(BfsError) as e:
+            moe_dispatch_workspace(4, 1, n_experts)
+        assert e.value.status == bfs.E_RESOURCE
     with pytest.raises(BfsError):
         GradSet([torch.zeros(3)])                     # not on a device
 
@@ -166,6 +173,23 @@ def test_grad_table(sizes):
     for b, r in enumerate(start):
         c = made.n_chunks * b // made.n_blocks
         assert r == rows[r[6]] and r[3] <= c < r[3] + r[4]
+
+
+@pytest.mark.parametrize("grads,outs,numel,dtypes,out_dtypes,overlap", [
+    ([A, A], [A, A], [4, 4], [F32, F32], [F32, F32], 1),                     # the same one twice, in place
+    ([A, A], [A + 64, A + 128], [4, 4], [F32, F32], [F32, F32], 0),          # ... to outputs of their own
+    ([A, A + 16], [A, A + 16], [4, 4], [F32, F32], [F32, F32], 0),           # neighbours in place
+    ([A, A + 12], [A, A + 12], [4, 4], [F32, F32], [F32, F32], 1),
+    ([A, A + 1024], [A + 4, A + 1024], [4, 4], [F32, F32], [F32, F32], 1),   # an output elsewhere in its gradient
+    ([A, A + 1024], [A + 1024, A + 2048], [4, 4], [F32, F32], [F32, F32], 1),  # an output on another gradient
+    ([A, A + 8], [A + 4096, A + 4112], [4, 4], [BF16, BF16], [F32, F32], 0),  # one flat output behind the gradients
+    ([A, A + 8], [A + 4096, A + 4108], [4, 4], [BF16, BF16], [F32, F32], 1),
+    ([A, A, None], [A + 64, A + 64, None], [4, 0, 0], [F32] * 3, [F32] * 3, 0),  # empty tensors overlap nothing
+    ([A + 512, A], [A + 512, A], [128, 128], [F32, F32], [F32, F32], 0),
+    ([A + 508, A], [A + 508, A], [128, 128], [F32, F32], [F32, F32], 1)])
+def test_grad_table_overlap(grads, outs, numel, dtypes, out_dtypes, overlap):
+    made, _ = _table(grads, outs, numel, dtypes, out_dtypes)
+    assert made.overlap == overlap
 
 
 def test_package_imports_without_the_operators():
