@@ -473,6 +473,7 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
 typedef struct {
   int64_t image_bytes;           /* device memory of the table */
   int64_t workspace_bytes;       /* device memory that a call works in */
+  int64_t grad_bytes;            /* the gradients' */
   int64_t chunk;                 /* the launches' shape, the library's own */
   int32_t n_entries, n_chunks, n_blocks;
   int32_t overlap;               /* not 0: outputs overlap, bfs_grad_clip refuses */

@@ -70,7 +70,7 @@ class RunOpts(C.Structure):
 
 
 class GradSetStruct(C.Structure):
-    _fields_ = [("image_bytes", C.c_int64), ("workspace_bytes", C.c_int64), ("chunk", C.c_int64), ("n_entries", C.c_int32),
+    _fields_ = [("image_bytes", C.c_int64), ("workspace_bytes", C.c_int64), ("grad_bytes", C.c_int64), ("chunk", C.c_int64), ("n_entries", C.c_int32),
                 ("n_chunks", C.c_int32), ("n_blocks", C.c_int32), ("overlap", C.c_int32)]
 
 

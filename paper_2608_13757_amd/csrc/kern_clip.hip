@@ -18,8 +18,9 @@
 // number (as launch arguments, 128 tensors a launch, 2^28 bf16 gradients in 290
 // tensors took six launches and 510 us).
 //
-// 2^28 bf16 gradients in 290 tensors into fp32: 405 us, 5.3 TB/s over both
-// passes, a large copy's rate; 2^20 fp32 in 24: 9 us, two short launches.
+// 2^28 bf16 gradients in 290 tensors into fp32: 387 us, 5.5 TB/s over both
+// passes (a large copy's rate is 5.3); 2^20 fp32 in 24: 8.5 us, two short
+// launches.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -34,10 +35,19 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnroll = 8;                        // accesses of a lane in flight
 // Elements a workgroup takes at once, less where the tensors would leave
-// workgroups idle (2^28 bf16 in 290 tensors: 405 us with 8192, 416 with 16384,
-// whose last chunks are less even over the workgroups, 427 with 4096).
+// workgroups idle (2^28 bf16 in 290 tensors: 389 us with 8192, 415 with 16384,
+// whose last chunks are less even over the workgroups).
 constexpr int64_t kMaxChunk = 8192, kMinChunk = 2048;
-constexpr int kBlocks = 1024;                     // workgroups at most (2048: 425 us there)
+// Workgroups: 1024, from four chunks for each of 4096 on these (clipping bf16,
+// 2^28: 410 us with 1024, 390 with 4096; 2^27: 198 and 189; 2^26: 91 and 97).
+// Numbers between leave a part of the device idle at the end (2^25 with 1030
+// of them 51 us, with 1024 48).
+constexpr int kBlocks = 1024, kMostBlocks = 4096, kChunksEach = 4;
+// Gradients' bytes from which the norm alone reads past the caches: they do not
+// fit the last-level one anyway (2^28 fp32: 206 us with plain loads, 182 with
+// these; 2^26 bf16: 27 and 30).  A clipping's first pass leaves there what it
+// can for the second.
+constexpr int64_t kStreamNorm = 256 << 20;
 constexpr int kLine = 128;                        // bytes of a cache line
 constexpr int64_t kMaxElements = (int64_t)1 << 43;
 constexpr double kEps = 1e-6;
@@ -64,6 +74,16 @@ struct Table {
 // Workgroup b of n runs chunks from .. to - 1.
 __device__ __forceinline__ int first_chunk(const Table &t, int b) { return (int)((int64_t)t.n_chunks * b / gridDim.x); }
 
+// The workgroup whose chunks this one scales: eight at a time in the opposite
+// order, where more run than are resident, and on the same of the eight XCDs
+// (workgroups go to them in turn), whose L2 still holds them after the first
+// pass.  2^23 bf16: 18.4 us in the plain opposite order, 15.7 so; 2^28: 389 and
+// 387; in the first pass's own order 15.5 and 424.
+__device__ __forceinline__ int opposite() {
+  const uint32_t n = gridDim.x, b = blockIdx.x;
+  return (int)(n % 8 ? b : (n - 8 - (b & ~7u)) | (b & 7u));
+}
+
 // Sum of s over the workgroup, in a fixed order, for every thread.
 __device__ __forceinline__ double block_sum(double s) {
   __shared__ double part[kThreads / kWave];
@@ -86,19 +106,22 @@ __device__ __forceinline__ int head_of(const T *p, int64_t n) {
 }
 
 // f on this lane's vectors while U accesses are whole, then with U / 2 of them.
-template <int U, typename Vec, int V, typename T, typename F>
+template <int U, bool kStream, typename Vec, int V, typename T, typename F>
 __device__ __forceinline__ void each_vector(const T *g, int64_t at, int64_t end, F f) {
   constexpr int kStep = kThreads * V;
   while (at + (U - 1) * kStep < end) {
     Vec v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Vec *>(g + at + u * kStep);
+    for (int u = 0; u < U; ++u) {
+      auto p = reinterpret_cast<const Vec *>(g + at + u * kStep);
+      v[u] = kStream ? __builtin_nontemporal_load(p) : *p;
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) f(at + u * kStep, v[u]);
     at += U * kStep;
     if (U < kUnroll) break;                       // fewer than U accesses are left
   }
-  if constexpr (U > 1) each_vector<U / 2, Vec, V>(g, at, end, f);
+  if constexpr (U > 1) each_vector<U / 2, kStream, Vec, V>(g, at, end, f);
 }
 
 // Chunk c of a tensor of n elements at g, `chunks` of them in all, whose first
@@ -107,23 +130,23 @@ __device__ __forceinline__ void each_vector(const T *g, int64_t at, int64_t end,
 // what is left.  f(first element, vector) for this lane's vectors, up to
 // kUnroll accesses issued before the first is used, one(element) for the
 // elements that no vector holds.
-template <typename Vec, int V, typename T, typename F, typename One>
+template <bool kStream, typename Vec, int V, typename T, typename F, typename One>
 __device__ __forceinline__ void each_element(const T *g, int64_t n, int head, int64_t chunk, int c, int chunks, F f, One one) {
   const int64_t from = head + c * chunk, to = c + 1 == chunks || from + chunk > n ? n : from + chunk;
   if (c == 0 && (int)threadIdx.x < head) one((int64_t)threadIdx.x);
   if (from >= to) return;
   const int64_t end = to - (to - from) % V;
-  each_vector<kUnroll, Vec, V>(g, from + (int64_t)threadIdx.x * V, end, f);
+  each_vector<kUnroll, kStream, Vec, V>(g, from + (int64_t)threadIdx.x * V, end, f);
   if (end + threadIdx.x < to) one(end + threadIdx.x);
 }
 
-template <typename T>
+template <bool kStream, typename T>
 __device__ __forceinline__ double square_sum(const Entry &e, int64_t chunk, int c) {
   constexpr int V = Chunk<T>::kElems;
   typedef typename Chunk<T>::vec vec;
   const T *g = static_cast<const T *>(e.in);
   double s = 0.0;
-  each_element<vec, V>(
+  each_element<kStream, vec, V>(
       g, e.n, head_of(g, e.n), chunk, c, e.chunks,
       [&](int64_t, vec v) {
 #pragma unroll
@@ -133,6 +156,7 @@ __device__ __forceinline__ double square_sum(const Entry &e, int64_t chunk, int 
   return s;
 }
 
+template <bool kStream>
 __global__ void __launch_bounds__(kThreads) square_kernel(Table t, double *partial) {
   const int from = first_chunk(t, (int)blockIdx.x), to = first_chunk(t, (int)blockIdx.x + 1);
   double s = 0.0;
@@ -140,9 +164,9 @@ __global__ void __launch_bounds__(kThreads) square_kernel(Table t, double *parti
   for (int c = from; c < to; ++c) {
     if (e.first + e.chunks <= c) e = t.entry[e.index + 1];
     switch (e.type & 15) {
-      case BFS_DTYPE_F32: s += square_sum<float>(e, t.chunk, c - e.first); break;
-      case BFS_DTYPE_BF16: s += square_sum<__bf16>(e, t.chunk, c - e.first); break;
-      default: s += square_sum<_Float16>(e, t.chunk, c - e.first); break;
+      case BFS_DTYPE_F32: s += square_sum<kStream, float>(e, t.chunk, c - e.first); break;
+      case BFS_DTYPE_BF16: s += square_sum<kStream, __bf16>(e, t.chunk, c - e.first); break;
+      default: s += square_sum<kStream, _Float16>(e, t.chunk, c - e.first); break;
     }
   }
   s = block_sum(s);
@@ -174,8 +198,8 @@ __device__ __forceinline__ Scale scale_of(double ratio) {
 // A lane's access is 16 bytes of the output, where the chunks begin with a
 // line: into a flat vector, in which tensors begin anywhere, whole lines are
 // written.  Nontemporal stores leave the last-level cache to the gradients that
-// the pass is still to read (2^25 fp32: 64 us with plain stores, 45 with these;
-// 2^23 and below: the same).
+// the pass is still to read (2^25 fp32, both passes: 85 us with plain stores, 64
+// with these; 2^23: 23 and 20).
 template <typename T, typename U>
 __device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c, Scale s) {
   constexpr int V = Chunk<U>::kElems;
@@ -183,7 +207,7 @@ __device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c
   typedef typename Chunk<U>::vec vec;
   const T *g = static_cast<const T *>(e.in);
   U *out = static_cast<U *>(e.out);
-  each_element<in_vec, V>(
+  each_element<false, in_vec, V>(
       g, e.n, head_of(out, e.n), chunk, c, e.chunks,
       [&](int64_t i, in_vec v) {
         vec o;
@@ -195,7 +219,7 @@ __device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c
 }
 
 __global__ void __launch_bounds__(kThreads) clip_kernel(Table t, const double *partial, double max_norm, float *norm) {
-  const int back = (int)(gridDim.x - 1 - blockIdx.x);
+  const int back = opposite();
   Entry e = t.start[back];                         // on its way under the sums
   const double root = sqrt(total_of(partial, (int)gridDim.x));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)root;
@@ -259,7 +283,7 @@ Table table_of(const bfs_grad_set &set, const void *image) {
 
 bfs_status check_call(const char *what, const bfs_grad_set *set, const void *image, const void *workspace, int64_t bytes) {
   if (!set) return fail(BFS_E_INVALID, std::string(what) + ": null set");
-  if (set->n_entries < 0 || set->n_chunks < set->n_entries || set->n_blocks < 0 || set->n_blocks > kBlocks ||
+  if (set->n_entries < 0 || set->n_chunks < set->n_entries || set->n_blocks < 0 || set->n_blocks > kMostBlocks ||
       (set->n_chunks > 0 && set->n_blocks < 1) || set->chunk < kMinChunk || set->chunk > kMaxChunk)
     return fail(BFS_E_INVALID, std::string(what) + ": not a set that bfs_grad_table made");
   if (set->n_chunks > 0 && (!image || (uintptr_t)image % 16)) return fail(BFS_E_INVALID, std::string(what) + ": bad table address");
@@ -278,7 +302,7 @@ bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int
   return entry([&]() -> bfs_status {
     if (n_tensors < 0 || !set || (n_tensors > 0 && (!grads || !outs || !numel || !dtypes || !out_dtypes)))
       return fail(BFS_E_INVALID, "grad_table: bad tensor list");
-    int64_t elements = 0;
+    int64_t elements = 0, bytes = 0;
     int32_t held = 0;
     for (int32_t i = 0; i < n_tensors; ++i) {
       if (numel[i] < 0) return fail(BFS_E_INVALID, "grad_table: negative tensor size");
@@ -292,6 +316,7 @@ bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int
         return fail(BFS_E_INVALID, "grad_table: a tensor is not aligned to its elements");
       if (numel[i] > kMaxElements || (elements += numel[i]) > kMaxElements)
         return fail(BFS_E_RESOURCE, "grad_table: more than 2^43 elements");
+      bytes += numel[i] * (dtypes[i] == BFS_DTYPE_F32 ? 4 : 2);
       held += numel[i] > 0;
     }
     bfs_grad_set s{};
@@ -300,9 +325,10 @@ bfs_status bfs_grad_table(const void *const *grads, void *const *outs, const int
     int64_t chunks = 0;
     for (int32_t i = 0; i < n_tensors; ++i) chunks += chunks_of(numel[i], s.chunk);
     if (chunks > INT32_MAX) return fail(BFS_E_RESOURCE, "grad_table: more than 2^31 - 1 chunks");
+    s.grad_bytes = bytes;
     s.n_entries = held;
     s.n_chunks = (int32_t)chunks;
-    s.n_blocks = chunks < kBlocks ? (int32_t)chunks : kBlocks;
+    s.n_blocks = chunks >= kMostBlocks * (int64_t)kChunksEach ? kMostBlocks : chunks < kBlocks ? (int32_t)chunks : kBlocks;
     s.workspace_bytes = (s.n_blocks > 0 ? s.n_blocks : 1) * (int64_t)sizeof(double);
     s.overlap = overlaps(grads, outs, numel, dtypes, out_dtypes, n_tensors);
     s.image_bytes = ((int64_t)held + s.n_blocks) * (int64_t)sizeof(Entry);
@@ -341,7 +367,8 @@ bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *
     if (st != BFS_OK) return st;
     double *partial = static_cast<double *>(workspace);
     if (set->n_blocks > 0)
-      st = launch("grad_norm", square_kernel, set->n_blocks, kThreads, 0, stream, table_of(*set, dev_image), partial);
+      st = launch("grad_norm", set->grad_bytes >= kStreamNorm ? square_kernel<true> : square_kernel<false>, set->n_blocks, kThreads,
+                  0, stream, table_of(*set, dev_image), partial);
     if (st != BFS_OK) return st;
     return launch("grad_norm", norm_kernel, 1, kThreads, 0, stream, partial, set->n_blocks, norm);
   });
@@ -358,7 +385,7 @@ bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double 
     double *partial = static_cast<double *>(workspace);
     if (set->n_blocks == 0) return norm ? launch("grad_clip", norm_kernel, 1, kThreads, 0, stream, partial, 0, norm) : BFS_OK;
     const Table t = table_of(*set, dev_image);
-    st = launch("grad_clip", square_kernel, set->n_blocks, kThreads, 0, stream, t, partial);
+    st = launch("grad_clip", square_kernel<false>, set->n_blocks, kThreads, 0, stream, t, partial);
     if (st != BFS_OK) return st;
     return launch("grad_clip", clip_kernel, set->n_blocks, kThreads, 0, stream,
                   t, partial, max_norm, norm);

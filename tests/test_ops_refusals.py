@@ -169,7 +169,8 @@ def test_grad_table(sizes):
     for _, _, size, first, chunks, _, _ in rows:
         assert first == at and (chunks - 1) * made.chunk < size <= chunks * made.chunk
         at += chunks
-    assert at == made.n_chunks and made.n_blocks == min(at, 1024) == len(start)
+    assert at == made.n_chunks and made.n_blocks == (4096 if at >= 16384 else min(at, 1024)) == len(start)
+    assert made.grad_bytes == 2 * sum(sizes)
     for b, r in enumerate(start):
         c = made.n_chunks * b // made.n_blocks
         assert r == rows[r[6]] and r[3] <= c < r[3] + r[4]
