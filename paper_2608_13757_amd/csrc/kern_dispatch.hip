@@ -12,15 +12,16 @@
 // adds the counts of the earlier batches, waves and groups of slots, so that
 // rows come in the same order in every run.  LDS atomics only count.
 //
-// The slots go in groups of up to 1024, a workgroup ranks a whole group.  Before
-// several groups one launch counts each group's slots by expert, and the
-// ranking workgroups sum the groups before theirs, or, where that table is long,
-// read sums that one more launch makes.  The rows are copied by the ranking
-// workgroups where 1024 of them give each wave one part of a row: several then
-// rank the same group, each for itself, and one launch is saved (2048 tokens of
-// 4096 bf16 to 8 experts each: 33.4 us, with the copy in a launch of its own
-// 35.6; 128 tokens to two: 5 us in a single launch).  Beyond, the copy is a
-// launch of its own, whose waves end with their stores under way.
+// The slots go in groups of up to 1024, a workgroup ranks a whole group.  Up to
+// 4096 slots it counts the other groups' too.  Beyond, one launch counts each
+// group's slots by expert, and the ranking workgroups sum the groups before
+// theirs, or, where that table is long, read sums that one more launch makes.
+// The rows are copied by the ranking workgroups where 1024 of them give each
+// wave one part of a row: several then rank the same group, each for itself,
+// and one launch is saved (2048 tokens of 4096 bf16 to 8 experts each: 33.4 us,
+// with the copy in a launch of its own 35.6; 128 tokens to two: 5 us in a single
+// launch).  Beyond, the copy is a launch of its own, whose waves end with their
+// stores under way.
 //
 // Bound by memory: 32768 tokens of 4096 bf16 to two experts of 64 each, 806 MB,
 // in 156 us (5.2 TB/s, a large copy's rate), some 8 us of them the ranking.
@@ -35,6 +36,10 @@ constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kBatches = 4;                            // batches of 64 slots per wave
 constexpr int kGroupSlots = kWaves * kBatches * kWave;
 constexpr int kBlocks = 1024;                          // workgroups that rank and copy, at most
+// Slots up to which every ranking workgroup counts all by itself (1000 tokens of
+// 1024 bf16 to two experts of 64: 6.7 us, with a launch that counts 8.4; 8000
+// slots: 15.8 and 12.6)
+constexpr int kAlone = 4096;
 constexpr int64_t kSumEntries = 8192;                  // counts that every workgroup sums by itself
 
 struct DispatchParams {
@@ -59,17 +64,60 @@ __device__ __forceinline__ void load_ids(const DispatchParams &P, int g, int wav
   }
 }
 
+// Counts the wave's ids in LDS (-1: none).  The first lane's id, which under a
+// skewed routing many share, is counted by one access for all of them: atomics
+// on one word run one lane after the other (4000 slots, most of them of two
+// experts, counted by every workgroup: 12.1 us without this, 8.7 with it).
+__device__ __forceinline__ void count_ids(uint32_t *counts, int id, int lane) {
+  const int first = __builtin_amdgcn_readfirstlane(id);
+  const uint64_t same = __ballot(id == first);
+  const bool one = lane == __builtin_ctzll(same);
+  if (id >= 0 && (id != first || one)) atomicAdd(&counts[id], one ? (uint32_t)__popcll(same) : 1u);
+}
+
 // Counts of each wave's slots by expert, then for each wave the slots of the
 // waves before it; total[e] the group's.  hist: [kWaves][n_experts], zeroed
-// here.
-__device__ __forceinline__ void count_waves(const DispatchParams &P, const int (&id)[kBatches], int wave, uint32_t *hist,
-                                            uint32_t *total) {
-  const int E = P.n_experts;
+// here.  Without a table of counts (up to kAlone slots) the other groups' slots
+// are counted too: before[e] of the groups before this one, after[e] behind it,
+// total[e] of all; others: after[n_experts + 1], then before[n_experts].
+__device__ __forceinline__ void count_waves(const DispatchParams &P, const int (&id)[kBatches], int g, int wave, int lane,
+                                            uint32_t *hist, uint32_t *total, uint32_t *others) {
+  typedef int32_t ids __attribute__((ext_vector_type(4), aligned(4)));
+  constexpr int kRounds = kAlone / (4 * kThreads);
+  const int E = P.n_experts, slots = (int)P.n_slots, first = g * P.group;
+  const bool alone = P.n_groups > 1 && !P.counts;
+  ids other[kRounds];
+  if (alone) {
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      if (r * kThreads * 4 >= slots) break;
+      const int s = (r * kThreads + (int)threadIdx.x) * 4;
+      if (s + 4 <= slots) {
+        other[r] = *reinterpret_cast<const ids *>(P.experts + s);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) other[r][i] = s + i < slots ? P.experts[s + i] : -1;
+      }
+    }
+    for (int i = (int)threadIdx.x; i < 2 * E + 1; i += kThreads) others[i] = 0;
+  }
   for (int i = (int)threadIdx.x; i < kWaves * E; i += kThreads) hist[i] = 0;
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < kBatches; ++b)
-    if (id[b] >= 0) atomicAdd(&hist[wave * E + id[b]], 1u);
+    count_ids(hist + wave * E, id[b], lane);
+  if (alone) {
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      if (r * kThreads * 4 >= slots) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int s = (r * kThreads + (int)threadIdx.x) * 4 + i;
+        const bool counts = (uint32_t)other[r][i] < (uint32_t)E && (uint32_t)(s - first) >= (uint32_t)P.group;
+        count_ids(others, counts ? other[r][i] + (s < first ? E + 1 : 0) : -1, lane);
+      }
+    }
+  }
   __syncthreads();
   for (int e = (int)threadIdx.x; e < E; e += kThreads) {
     uint32_t run = 0;
@@ -79,7 +127,7 @@ __device__ __forceinline__ void count_waves(const DispatchParams &P, const int (
       hist[w * E + e] = run;
       run += c;
     }
-    total[e] = run;
+    total[e] = alone ? run + others[e] + others[E + 1 + e] : run;
   }
   __syncthreads();
 }
@@ -202,8 +250,8 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(DispatchParams P) {
   const int64_t first = (int64_t)g * P.group;
   int id[kBatches], row[kBatches];
   load_ids(P, g, wave, lane, id);
-  count_waves(P, id, wave, hist, total);
-  if (P.n_groups > 1) sum_groups(P, g, before, total);
+  count_waves(P, id, g, wave, lane, hist, total, start);
+  if (P.counts) sum_groups(P, g, before, total);
   expert_starts(E, total, start, wave, lane);
   if (P.n_groups > 1) {
     for (int e = (int)threadIdx.x; e < E; e += kThreads) before[e] += start[e];
@@ -251,7 +299,7 @@ __global__ void __launch_bounds__(kThreads) count_kernel(DispatchParams P) {
   __syncthreads();
 #pragma unroll
   for (int b = 0; b < kBatches; ++b)
-    if (id[b] >= 0) atomicAdd(&lds[id[b]], 1u);
+    count_ids(lds, id[b], lane);
   __syncthreads();
   for (int e = (int)threadIdx.x; e < P.n_experts; e += kThreads) P.counts[(int64_t)blockIdx.x * P.n_experts + e] = lds[e];
 }
@@ -282,7 +330,7 @@ int32_t group_of(int32_t k) { return kGroupSlots / k * k; }
 int64_t groups_of(int64_t slots, int32_t k) { return (slots + group_of(k) - 1) / group_of(k); }
 int64_t counts_of(int64_t slots, int32_t k, int32_t n_experts) {
   const int64_t groups = groups_of(slots, k);
-  return groups <= 1 ? 0 : (groups + 1) * n_experts * (int64_t)sizeof(uint32_t);
+  return slots <= kAlone ? 0 : (groups + 1) * n_experts * (int64_t)sizeof(uint32_t);
 }
 
 bfs_status check_sizes(const char *what, int64_t n_tokens, int32_t k, int32_t n_experts) {
@@ -330,7 +378,7 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
     P.off = expert_off;
     P.pos = pos;
     P.rows = rows;
-    P.counts = static_cast<uint32_t *>(workspace);
+    P.counts = need > 0 ? static_cast<uint32_t *>(workspace) : nullptr;
     P.n_slots = slots;
     P.x_stride = x_stride;
     P.rows_stride = rows_stride;
@@ -344,8 +392,8 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
     auto copy = [&](auto t) -> bfs_status {
       using T = decltype(t);
       bfs_status s = BFS_OK;
-      if (groups > 1) s = launch("moe_dispatch", count_kernel, groups, kThreads, n_experts * sizeof(uint32_t), stream, P);
-      if (s == BFS_OK && groups > 1 && groups * n_experts > kSumEntries)
+      if (need > 0) s = launch("moe_dispatch", count_kernel, groups, kThreads, n_experts * sizeof(uint32_t), stream, P);
+      if (s == BFS_OK && need > 0 && groups * n_experts > kSumEntries)
         s = launch("moe_dispatch", sum_kernel, (n_experts + kWaves - 1) / kWaves, kThreads, 0, stream, P);
       if (s != BFS_OK) return s;
       const size_t lds = ((kWaves + 3) * (size_t)n_experts + 1 + kGroupSlots) * sizeof(uint32_t);

@@ -27,7 +27,7 @@ from .bfs import E_INVALID, E_RESOURCE, OK, BfsError
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOE_RENORMALIZE = 1
 MAX_EXPERTS = 1024
-DISPATCH_ONE_GROUP = 1024        # slots of one group: at most one needs no workspace
+DISPATCH_ALONE = 4096            # slots up to which a dispatch needs no workspace
 _I32, _F32 = torch.int32, torch.float32
 
 # The current device and its current stream's handle, by the bindings that
@@ -179,10 +179,10 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         _refuse_experts(name, n_experts)
     t, k = shape
     slots = t * k
-    one_group = k and slots <= DISPATCH_ONE_GROUP // k * k
+    alone = k and slots <= DISPATCH_ALONE
     handle = _raw_stream(device) if stream is None else _stream(
         name, stream, device, perm is not None and expert_off is not None and pos is not None
-        and (x is None or rows is not None) and (one_group or workspace is not None))
+        and (x is None or rows is not None) and (alone or workspace is not None))
     if perm is None:
         perm = experts.new_empty(slots)
     elif perm.dtype is not _I32 or perm.shape != (slots,) or perm.get_device() != device or not perm.is_contiguous():
@@ -221,7 +221,7 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         x_ptr, rows_ptr = x.data_ptr(), rows.data_ptr()
     elif rows is not None:
         _refuse(name, "rows without x")
-    if not one_group:
+    if not alone:
         if workspace is None:
             workspace = experts.new_empty(moe_dispatch_workspace(t, k, n_experts), dtype=torch.uint8)
         elif workspace.get_device() != device or not workspace.is_contiguous():

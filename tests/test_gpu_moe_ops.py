@@ -255,10 +255,10 @@ def _dispatch_reference(experts, e):
     return slots // experts.shape[1], off, pos.reshape(experts.shape)
 
 
-# around one wave's batch, one launch's limit (1024 slots) and one group (4096)
+# around one wave's batch, one group (1024 slots) and one launch's limit (4096)
 DISPATCH = [(0, 2, 5, 8), (1, 1, 1, 1), (1, 8, 64, 4096), (3, 1, 5, 7), (8, 2, 64, 130), (63, 1, 3, 16), (65, 1, 1, 33),
             (128, 8, 64, 24), (1024, 1, 17, 8), (1025, 1, 17, 9), (512, 2, 1024, 12), (342, 3, 300, 65), (4096, 1, 64, 4),
-            (4097, 1, 64, 3), (1500, 7, 256, 40), (9001, 4, 33, 17), (2, 64, 100, 20), (300, 64, 1000, 8)]
+            (4097, 1, 64, 3), (1500, 7, 256, 40), (9001, 4, 33, 17), (1365, 3, 90, 11), (1366, 3, 90, 11), (511, 5, 1024, 6), (585, 7, 2, 19), (2047, 2, 700, 5), (2, 64, 100, 20), (300, 64, 1000, 8)]
 
 
 @pytest.mark.parametrize("t,k,e,h", DISPATCH)

@@ -76,8 +76,8 @@ INVALID = [
     (_dispatch, dict(t=-1)), (_dispatch, dict(k=0)), (_dispatch, dict(e=0)), (_dispatch, dict(experts=None)),
     (_dispatch, dict(perm=None)), (_dispatch, dict(off=None)), (_dispatch, dict(pos=None)), (_dispatch, dict(x=None)),
     (_dispatch, dict(rows=None)), (_dispatch, dict(width=-1)), (_dispatch, dict(rows_stride=15)),
-    (_dispatch, dict(x_stride=-16)), (_dispatch, dict(dtype=3)), (_dispatch, dict(t=4096)),
-    (_dispatch, dict(t=4096, ws=A, ws_bytes=4)), (_dispatch, dict(t=4096, ws=A + 2, ws_bytes=1 << 20)),
+    (_dispatch, dict(x_stride=-16)), (_dispatch, dict(dtype=3)), (_dispatch, dict(t=1 << 14)),
+    (_dispatch, dict(t=1 << 14, ws=A, ws_bytes=4)), (_dispatch, dict(t=1 << 14, ws=A + 2, ws_bytes=1 << 20)),
     (_combine, dict(n=-1)), (_combine, dict(width=-1)), (_combine, dict(t=-1)), (_combine, dict(k=0)),
     (_combine, dict(stride=-1)), (_combine, dict(y_stride=15)), (_combine, dict(dtype=3)), (_combine, dict(pos=None)),
     (_combine, dict(y=None)), (_combine, dict(rows=None)),
@@ -129,9 +129,9 @@ def test_nothing_to_do():
 def test_workspaces():
     torch = pytest.importorskip("torch")
     from paper_2608_13757_amd import GradSet, moe_dispatch_workspace
-    from paper_2608_13757_amd.ops import DISPATCH_ONE_GROUP
+    from paper_2608_13757_amd.ops import DISPATCH_ALONE
     for k in (1, 2, 3, 7, 64):
-        most = DISPATCH_ONE_GROUP // k
+        most = DISPATCH_ALONE // k
         assert moe_dispatch_workspace(0, k, 64) == 0 and moe_dispatch_workspace(most, k, 64) == 0
         assert moe_dispatch_workspace(most + 1, k, 64) > 0
     assert moe_dispatch_workspace(32768, 2, 64) > 0
