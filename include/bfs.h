@@ -499,6 +499,24 @@ bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *
 bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double max_norm, float *norm, void *workspace,
                          int64_t workspace_bytes, struct ihipStream_t *stream);
 
+/*
+ * Any of these calls with its arguments in an array: words[0] the operator,
+ * words[1] the number of its parameters, then these in their order, addresses
+ * and integers as 64-bit integers, a double by its bits.  An integer that its
+ * parameter's type does not hold is BFS_E_INVALID.  For bindings that convert
+ * arguments one by one.
+ */
+enum {
+  BFS_CALL_MOE_ROUTE = 0,
+  BFS_CALL_MOE_ROUTE_GRAD = 1,
+  BFS_CALL_MOE_DISPATCH = 2,
+  BFS_CALL_MOE_COMBINE = 3,
+  BFS_CALL_MOE_COMBINE_GRAD = 4,
+  BFS_CALL_GRAD_NORM = 5,
+  BFS_CALL_GRAD_CLIP = 6
+};
+bfs_status bfs_call(const int64_t *words);
+
 const char *bfs_status_string(bfs_status s);
 const char *bfs_last_error(void);
 

@@ -26,7 +26,7 @@ KERNELS = {"interp": 0, "stream3": 1, "gemm": 2, "attn": 3, "moe": 4, "rmsnorm":
 EXPORTED = ["bfs_plan_create", "bfs_plan_formulas", "bfs_plan_static_waits", "bfs_plan_stats",
             "bfs_eval_threshold", "bfs_plan_destroy", "bfs_run", "bfs_run_noalloc", "bfs_run_status",
             "bfs_moe_route", "bfs_moe_route_grad", "bfs_moe_dispatch_workspace", "bfs_moe_dispatch", "bfs_moe_combine",
-            "bfs_moe_combine_grad", "bfs_grad_table", "bfs_grad_norm", "bfs_grad_clip",
+            "bfs_moe_combine_grad", "bfs_grad_table", "bfs_grad_norm", "bfs_grad_clip", "bfs_call",
             "bfs_status_string", "bfs_last_error"]
 
 
@@ -119,7 +119,8 @@ def lib():
                 ("bfs_moe_combine_grad", [p, i32, i64, i64, i64, p, i64, i64, p, p, i32, p, i64, p, p]),
                 ("bfs_grad_table", [p, p, p, p, p, i32, p, p, i64]),
                 ("bfs_grad_norm", [p, p, p, p, i64, p]),
-                ("bfs_grad_clip", [p, p, C.c_double, p, p, i64, p])):
+                ("bfs_grad_clip", [p, p, C.c_double, p, p, i64, p]),
+                ("bfs_call", [p])):
             getattr(L, name).restype = C.c_int
             getattr(L, name).argtypes = args
         L.bfs_status_string.restype = C.c_char_p

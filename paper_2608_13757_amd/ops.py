@@ -28,6 +28,9 @@ DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOE_RENORMALIZE = 1
 MAX_EXPERTS = 1024
 DISPATCH_ALONE = 4096            # slots up to which a dispatch needs no workspace
+# bfs_call's words: the operator, the number of its arguments, the arguments
+_ROUTE, _ROUTE_GRAD, _DISPATCH, _COMBINE, _COMBINE_GRAD, _NORM, _CLIP = (
+    struct.Struct(f).pack for f in ("12q", "14q", "18q", "14q", "17q", "8q", "4qd4q"))
 _I32, _F32 = torch.int32, torch.float32
 
 # The current device and its current stream's handle, by the bindings that
@@ -108,9 +111,9 @@ def moe_route(logits, k, *, renormalize=True, experts=None, weights=None, stream
         weights = logits.new_empty(shape, dtype=_F32)
     elif weights.dtype is not _F32 or weights.shape != shape or weights.get_device() != device or not weights.is_contiguous():
         _refuse_dense(name, "weights", weights, shape, _F32)
-    status = (bfs._lib or bfs.lib()).bfs_moe_route(
-        logits.data_ptr(), dtype, t, e, stride, k, MOE_RENORMALIZE if renormalize else 0, experts.data_ptr(),
-        weights.data_ptr(), handle)
+    status = (bfs._lib or bfs.lib()).bfs_call(_ROUTE(
+        0, 10, logits.data_ptr(), dtype, t, e, stride, k, MOE_RENORMALIZE if renormalize else 0, experts.data_ptr(),
+        weights.data_ptr(), handle))
     if status:
         bfs._check(status)
     return experts, weights
@@ -145,9 +148,9 @@ def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logi
     out_stride, unit = grad_logits.stride()
     if (unit != 1 and e > 1) or (out_stride < e and t > 1):
         _refuse_like(name, "grad_logits", grad_logits, size, logits.dtype)
-    status = (bfs._lib or bfs.lib()).bfs_moe_route_grad(
-        logits.data_ptr(), dtype, t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
-        MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride if t > 1 else e, handle)
+    status = (bfs._lib or bfs.lib()).bfs_call(_ROUTE_GRAD(
+        1, 12, logits.data_ptr(), dtype, t, e, stride, experts.data_ptr(), k, grad_weights.data_ptr(),
+        MOE_RENORMALIZE if renormalize else 0, grad_logits.data_ptr(), out_stride if t > 1 else e, handle))
     if status:
         bfs._check(status)
     return grad_logits
@@ -196,8 +199,7 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         pos = experts.new_empty(shape)
     elif pos.dtype is not _I32 or pos.shape != shape or pos.get_device() != device or not pos.is_contiguous():
         _refuse_dense(name, "pos", pos, shape, _I32)
-    x_ptr = rows_ptr = ws_ptr = None
-    dtype = width = x_stride = rows_stride = ws_bytes = 0
+    x_ptr = rows_ptr = ws_ptr = dtype = width = x_stride = rows_stride = ws_bytes = 0
     if x is not None:
         size = x.shape
         if x.get_device() != device or len(size) != 2 or size[0] != t:
@@ -227,9 +229,9 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         elif workspace.get_device() != device or not workspace.is_contiguous():
             _refuse(name, "workspace must be a contiguous tensor on the current device")
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    status = (bfs._lib or bfs.lib()).bfs_moe_dispatch(
-        experts.data_ptr(), t, k, n_experts, perm.data_ptr(), expert_off.data_ptr(), pos.data_ptr(), x_ptr, dtype, width,
-        x_stride, rows_ptr, rows_stride, ws_ptr, ws_bytes, handle)
+    status = (bfs._lib or bfs.lib()).bfs_call(_DISPATCH(
+        2, 16, experts.data_ptr(), t, k, n_experts, perm.data_ptr(), expert_off.data_ptr(), pos.data_ptr(), x_ptr, dtype, width,
+        x_stride, rows_ptr, rows_stride, ws_ptr, ws_bytes, handle))
     if status:
         bfs._check(status)
     return perm, expert_off, pos, rows
@@ -249,7 +251,7 @@ def _combine(name, rows, pos, weights, out, stream):
     if pos.dtype is not _I32 or len(shape) != 2 or pos.get_device() != device or not pos.is_contiguous():
         _refuse(name, f"pos must be a contiguous int32 matrix on the current device, not {pos.dtype} {tuple(shape)}")
     t, k = shape
-    w_ptr = None
+    w_ptr = 0
     if weights is not None:
         if weights.dtype is not _F32 or weights.shape != shape or weights.get_device() != device or not weights.is_contiguous():
             _refuse_dense(name, "weights", weights, shape, _F32)
@@ -262,9 +264,9 @@ def _combine(name, rows, pos, weights, out, stream):
     out_stride, unit = out.stride()
     if (unit != 1 and width > 1) or (out_stride < width and t > 1):
         _refuse_like(name, "out", out, (t, width), rows.dtype)
-    status = (bfs._lib or bfs.lib()).bfs_moe_combine(
-        rows.data_ptr(), dtype, n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(), out_stride if t > 1 else width,
-        handle)
+    status = (bfs._lib or bfs.lib()).bfs_call(_COMBINE(
+        3, 12, rows.data_ptr(), dtype, n, width, stride, pos.data_ptr(), w_ptr, t, k, out.data_ptr(),
+        out_stride if t > 1 else width, handle))
     if status:
         bfs._check(status)
     return out
@@ -325,9 +327,9 @@ def moe_combine_grad(grad_y, rows, pos, weights, *, grad_rows=None, grad_weights
     elif (grad_weights.dtype is not _F32 or grad_weights.shape != slots or grad_weights.get_device() != device
           or not grad_weights.is_contiguous()):
         _refuse_dense(name, "grad_weights", grad_weights, slots, _F32)
-    status = (bfs._lib or bfs.lib()).bfs_moe_combine_grad(
-        grad_y.data_ptr(), dtype, t, width, dy_stride, rows.data_ptr(), n, rows_stride, pos.data_ptr(), weights.data_ptr(), k,
-        grad_rows.data_ptr(), out_stride if n > 1 else width, grad_weights.data_ptr(), handle)
+    status = (bfs._lib or bfs.lib()).bfs_call(_COMBINE_GRAD(
+        4, 15, grad_y.data_ptr(), dtype, t, width, dy_stride, rows.data_ptr(), n, rows_stride, pos.data_ptr(), weights.data_ptr(),
+        k, grad_rows.data_ptr(), out_stride if n > 1 else width, grad_weights.data_ptr(), handle))
     if status:
         bfs._check(status)
     return grad_rows, grad_weights
@@ -391,7 +393,7 @@ class GradSet:
             image = bytearray(size)
             _call(table, *arrays, C.byref(self._set), (C.c_char * size).from_buffer(image), size)
             self._table = torch.frombuffer(image, dtype=torch.uint8).to(grads[0].device)     # waits for the copy
-        self._args = C.byref(self._set), None if self._table is None else self._table.data_ptr()
+        self._args = C.addressof(self._set), 0 if self._table is None else self._table.data_ptr()
         self.workspace_bytes = self._set.workspace_bytes
 
     def _buffers(self, name, norm, workspace, stream):
@@ -413,7 +415,7 @@ class GradSet:
     def norm(self, norm=None, workspace=None, stream=None):
         """The global norm, a float32 scalar on the device."""
         norm, workspace, size, handle = self._buffers("grad_norm", norm, workspace, stream)
-        _call(bfs._lib.bfs_grad_norm, *self._args, norm.data_ptr(), workspace.data_ptr(), size, handle)
+        _call(bfs._lib.bfs_call, _NORM(5, 6, *self._args, norm.data_ptr(), workspace.data_ptr(), size, handle))
         return norm
 
     def clip(self, max_norm, norm=None, workspace=None, stream=None):
@@ -421,7 +423,7 @@ class GradSet:
         returns the norm before clipping.  A norm that is not finite (in
         float32) scales by 1."""
         norm, workspace, size, handle = self._buffers("grad_clip", norm, workspace, stream)
-        _call(bfs._lib.bfs_grad_clip, *self._args, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle)
+        _call(bfs._lib.bfs_call, _CLIP(6, 7, *self._args, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle))
         return norm
 
 

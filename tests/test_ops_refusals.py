@@ -14,8 +14,11 @@ A = 1 << 20                     # an address that no call uses
 F32, BF16, F16 = 0, 1, 2
 
 
-def _status(name, *args):
+def _named(name, *args):
     return getattr(bfs.lib(), name)(*args)
+
+
+_status = _named
 
 
 def _route(logits=A, dtype=F32, t=4, e=8, stride=8, k=2, flags=1, experts=A, weights=A):
@@ -101,6 +104,36 @@ INVALID = [
 def test_invalid_arguments(call, kw):
     assert call(**kw) == bfs.E_INVALID
     assert bfs.lib().bfs_last_error()
+
+
+CALLS = {"bfs_moe_route": (0, "PqqqqqqPPP"), "bfs_moe_route_grad": (1, "PqqqqPqPqPqP"), "bfs_moe_dispatch": (2, "PqqqPPPPqqqPqPqP"),
+         "bfs_moe_combine": (3, "PqqqqPPqqPqP"), "bfs_moe_combine_grad": (4, "PqqqqPqqPPqPqPP"), "bfs_grad_norm": (5, "PPPPqP"),
+         "bfs_grad_clip": (6, "PPdPPqP")}
+
+
+def _words(name, *args):
+    op, kinds = CALLS[name]
+    values = [C.addressof(a._obj) if hasattr(a, "_obj") else 0 if a is None else a for a in args]
+    return bfs.lib().bfs_call(struct.pack("qq" + kinds, op, len(kinds), *values))
+
+
+@pytest.mark.parametrize("call,kw", [c for c in INVALID if c[0] is not _table], ids=lambda v: getattr(v, "__name__", str(v)))
+def test_invalid_arguments_as_words(call, kw, monkeypatch):
+    monkeypatch.setattr(sys.modules[__name__], "_status", lambda name, *a: (_words if name in CALLS else _named)(name, *a))
+    assert call(**kw) == bfs.E_INVALID
+    assert bfs.lib().bfs_last_error()
+
+
+def test_words():
+    """The array itself: its operator, its count, integers that do not fit."""
+    call = bfs.lib().bfs_call
+    assert call(None) == bfs.E_INVALID
+    for op, n, extra in ((-1, 0, ""), (7, 0, ""), (0, 9, "10q"), (0, 11, "11q"), (2, 10, "16q")):
+        assert call(struct.pack("qq" + extra, op, n, *[0] * (int(extra[:-1]) if extra else 0))) == bfs.E_INVALID
+    route = [A, F32, 0, 8, 8, 2, 1, A, A, 0]                     # no tokens: nothing to do
+    assert call(struct.pack("12q", 0, 10, *route)) == bfs.OK
+    for i, bad in ((1, 1 << 32), (3, (1 << 32) + 8), (5, (1 << 32) + 2), (5, -(1 << 31) - 1), (6, 1 << 32), (6, -1)):
+        assert call(struct.pack("12q", 0, 10, *[bad if j == i else v for j, v in enumerate(route)])) == bfs.E_INVALID
 
 
 RESOURCE = [(_route, dict(e=1025, stride=1025)), (_route, dict(e=64, stride=64, k=17)), (_route, dict(t=1 << 31)),
