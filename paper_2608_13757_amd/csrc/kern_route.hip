@@ -18,19 +18,21 @@
 // for a whole wave).  Logits are compared as unsigned keys in the order of the
 // floats, -0 as +0, NaN above everything.  A 16-bit logit's key and its
 // expert's number make one word, all different, so that a maximum finds the
-// lowest of equal ones by itself; of fp32 logits the lanes that hold the maximum
-// are counted, and only rows with several of them take another reduction.
+// lowest of equal ones by itself; of fp32 logits the upper part of the key does
+// (select), or the lanes that hold the maximum are counted.
 //
 // The softmax is in fp32 whatever the logits' type; exponentials are exp2 of
-// the product with log2 e, off by some 2 |z - m| 2^-24, which is less the larger
-// they are.
+// the product with log2 e, off by some 2 |z - m| 2^-24 relative to themselves;
+// weights below fp32's normal numbers become 0.
 //
-// Bound by instructions for many tokens (k rounds of a maximum): 32768 tokens,
-// 64 experts, k = 8, bf16: 5.2 us, where reading and writing would take 1.2; the
-// gradient of 16384 tokens, 256 experts, fp32: 8.6 us (6.8).  With equal keys
-// found by a second reduction in every round, and the k terms of the gradient
-// compared with every expert, 6.6 and 11.5.
+// Bound by instructions for many tokens (k rounds of a maximum).  32768 tokens,
+// k = 8: 64 experts, bf16: 4.3 us, where reading and writing would take 1.2
+// (4.9 with a maximum over all values of a lane in every round, 6.6 with equal
+// keys found by a second reduction); 256 experts: bf16 9.5 us (11.7, reading 3.2),
+// fp32 12.0 (15.3, reading 6.3).  The gradient of 16384 tokens, 256 experts, fp32:
+// 8.6 us (6.8; 11.5 with the k terms compared with every expert).
 #include <cmath>
+#include <utility>
 
 #include "op_common.h"
 
@@ -48,7 +50,6 @@ struct Key;
 
 template <>
 struct Key<float> {
-  static constexpr bool kUnique = false;
   static constexpr uint32_t kMasked = 0x007fffffu, kNan = 0xffffffffu;
   __device__ static uint32_t of(float z, int) {
     if (z != z) return kNan;
@@ -61,7 +62,6 @@ struct Key<float> {
 // The logit's 16 bits above the expert's number from 65535 down.
 template <typename T>
 struct Key16 {
-  static constexpr bool kUnique = true;
   __device__ static uint32_t of(float z, int e) {
     const uint32_t u = __builtin_bit_cast(uint16_t, (T)(z + 0.0f));
     const uint32_t k = z != z ? 0xffffu : u ^ (u & 0x8000u ? 0xffffu : 0x8000u);
@@ -112,79 +112,193 @@ __device__ __forceinline__ void load_row(const T *row, int l, int n_experts, flo
   }
 }
 
-// The k largest keys of each group, taken out of `key`: in lane j < k the j-th
-// key and its expert; top: the largest.
-template <typename T, int G, int N>
-__device__ __forceinline__ void select(uint32_t (&key)[N], int l, int k, uint32_t &my_key, int &my_expert, uint32_t &top) {
-  using L = Layout<G, N>;
-  my_key = top = 0;
-  my_expert = -1;
-  if constexpr (Key<T>::kUnique) {
-    for (int j = 0; j < k; ++j) {
-      uint32_t m = key[0];
+// Batcher's odd-even merging network for N values: `n` comparisons of a[] < b[].
+template <int N>
+struct Network {
+  int a[64] = {}, b[64] = {}, n = 0;
+  constexpr Network() {
+    for (int p = 1; p < N; p <<= 1)
+      for (int q = p; q >= 1; q >>= 1)
+        for (int j = q % p; j + q < N; j += 2 * q)
+          for (int i = j; i < j + q && i + q < N; ++i)
+            if (i / (2 * p) == (i + q) / (2 * p)) {
+              a[n] = i;
+              b[n++] = i + q;
+            }
+  }
+};
+
+// v in descending order.
+template <int N, size_t... I>
+__device__ __forceinline__ void sort_down(uint32_t (&v)[N], std::index_sequence<I...>) {
+  constexpr Network<N> net{};
+  auto order = [](uint32_t &x, uint32_t &y) {
+    const uint32_t hi = x > y ? x : y, lo = x > y ? y : x;
+    x = hi;
+    y = lo;
+  };
+  (order(v[net.a[I]], v[net.b[I]]), ...);
+}
+
+// The `rounds` <= R largest of each group's keys, all different but for 0:
+// lane j gets the j-th, every lane the first (`most`), the last one, and the one
+// before it.  Each
+// lane sorts its own, so that a round looks at the lanes' first ones alone; of
+// what is behind them only as many as there are rounds left move up.
+template <int G, int N, int R, int J = 0>
+__device__ __forceinline__ void take_rounds(uint32_t (&key)[N], int l, int rounds, uint32_t &mine, uint32_t &most, uint32_t &last,
+                                            uint32_t &before) {
+  if constexpr (J < R) {
+    if (J >= rounds) return;
+    const uint32_t m = group_max<G>(key[0]);
+    const bool hit = key[0] == m;
 #pragma unroll
-      for (int i = 1; i < N; ++i) m = key[i] > m ? key[i] : m;
-      m = group_max<G>(m);
-      if (j == 0) top = m;
-#pragma unroll
-      for (int i = 0; i < N; ++i) key[i] = key[i] == m ? 0u : key[i];
-      my_key = l == j ? m : my_key;
-    }
-    if (my_key > Key<T>::kMasked) my_expert = Key<T>::expert(my_key);
-  } else {
-    // the lane that holds the maximum leaves it and its expert for lane j
-    __shared__ uint2 found[kThreads / G][kMaxK];
-    uint2 *mine = found[threadIdx.x / G];
-    for (int j = 0; j < k; ++j) {
-      uint32_t own = key[0];
-#pragma unroll
-      for (int i = 1; i < N; ++i) own = key[i] > own ? key[i] : own;
-      const uint32_t m = group_max<G>(own);
-      if (j == 0) top = m;
-      bool has = own == m;
-      if (__builtin_popcountll(__ballot(has)) != kWave / G) {      // several lanes of a row: the lowest expert
-        uint32_t e = 0x7fffffffu;
-#pragma unroll
-        for (int i = N - 1; i >= 0; --i) e = key[i] == m ? (uint32_t)L::index(l, i) : e;
-        has = e == group_min<G>(e);
-      }
-      uint32_t e = 0;
-      bool left = has;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {                                // experts ascend: the first of equal ones
-        const bool hit = left && key[i] == m;
-        key[i] = hit ? 0u : key[i];
-        e = hit ? (uint32_t)L::index(l, i) : e;
-        left = left && !hit;
-      }
-      if (has) mine[j] = make_uint2(m, e);
-    }
-    wave_sync();
-    if (l < k) {
-      const uint2 f = mine[l];
-      my_key = f.x;
-      if (f.x > Key<T>::kMasked) my_expert = (int)f.y;
-    }
+    for (int i = 0; i < (N < R - 1 - J ? N : R - 1 - J); ++i) key[i] = hit ? (i + 1 < N ? key[i + 1] : 0u) : key[i];
+    mine = l == J ? m : mine;
+    if (J == 0) most = m;
+    before = last;
+    last = m;
+    take_rounds<G, N, R, J + 1>(key, l, rounds, mine, most, last, before);
   }
 }
 
-template <typename T, int G, int N>
+template <int G, int N, int R>
+__device__ __forceinline__ uint32_t take_largest(uint32_t (&key)[N], int l, int rounds, uint32_t &most, uint32_t &last, uint32_t &before) {
+  sort_down(key, std::make_index_sequence<(size_t)Network<N>{}.n>{});
+  uint32_t mine = most = last = before = 0;
+  take_rounds<G, N, R>(key, l, rounds, mine, most, last, before);
+  return mine;
+}
+
+// Lane J's value of each group, for all its lanes.
+template <int G, int J>
+__device__ __forceinline__ uint32_t group_read(uint32_t x) {
+  if (G == 64) return (uint32_t)__builtin_amdgcn_readlane((int)x, J);
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + J, 0xf, 0xf, false);       // row_newbcast
+}
+
+// Exact for any fp32 keys: a maximum in each round, and the lowest of the
+// experts that hold it; with kCount these are looked for only where several
+// lanes of a row hold it (fewer instructions, more registers).  In lane j < k
+// the j-th key and its expert, -1 without one; top: the largest key.
+template <int G, int N, bool kCount>
+__device__ __forceinline__ int select_ties(uint32_t (&key)[N], int l, int k, uint32_t &my_key, uint32_t &top) {
+  using L = Layout<G, N>;
+  // the lane that holds the maximum leaves it and its expert for lane j
+  __shared__ uint2 found[kThreads / G][kMaxK];
+  uint2 *mine = found[threadIdx.x / G];
+  for (int j = 0; j < k; ++j) {
+    uint32_t own = key[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) own = key[i] > own ? key[i] : own;
+    const uint32_t m = group_max<G>(own);
+    if (j == 0) top = m;
+    bool has = own == m;
+    uint32_t e = 0;
+    if (!kCount || __builtin_popcountll(__ballot(has)) != kWave / G) {
+      e = 0x7fffffffu;
+#pragma unroll
+      for (int i = N - 1; i >= 0; --i) e = key[i] == m ? (uint32_t)L::index(l, i) : e;
+      has = e == group_min<G>(e);
+    }
+    bool left = has;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {                                  // experts ascend: the first of equal ones
+      const bool hit = left && key[i] == m;
+      key[i] = hit ? 0u : key[i];
+      if (kCount) e = hit ? (uint32_t)L::index(l, i) : e;
+      left = left && !hit;
+    }
+    if (has) mine[j] = make_uint2(m, e);
+  }
+  wave_sync();
+  const uint2 f = l < k ? mine[l] : make_uint2(0, 0);
+  my_key = f.x;
+  return f.x > Key<float>::kMasked ? (int)f.y : -1;
+}
+
+// Whether a row is sorted.  fp32 rows of few values a lane, or of which few are
+// wanted, go by their whole keys at once (32768 tokens: 64 experts, k = 4: 4.4
+// us, sorted 4.5; 256, k = 2: 8.7 and 8.8, k = 4: 10.7 and 9.4).
+template <typename T, int N, int K>
+constexpr bool kSorts = sizeof(T) == 2 || (N >= 8 && K > 2);
+
+// The k largest logits of each group's row: in lane j < k the j-th's expert
+// and value (-1 and -inf without one), in every lane the largest value.
+// fp32 logits are compared by what of a key stands above the bits of the
+// expert's number, then the chosen ones read again: where two of them, or the
+// last and any that is left, agree in that part and not in the whole (a few in
+// a hundred rows of random logits), the wave takes the exact way.
+template <typename T, int G, int N, int K>
+__device__ __forceinline__ void select(const T *row, const float (&z)[N], int l, int n_experts, int k, int &my_expert,
+                                       float &my_value, float &top) {
+  using L = Layout<G, N>;
+  uint32_t key[N], most, last, before;
+  my_expert = -1;
+  my_value = -INFINITY;
+  auto whole_keys = [&] {
+#pragma unroll
+    for (int i = 0; i < N; ++i) key[i] = L::index(l, i) < n_experts ? Key<T>::of(z[i], L::index(l, i)) : 0u;
+  };
+  if constexpr (!kSorts<T, N, K>) {
+    uint32_t mine, most;
+    whole_keys();
+    my_expert = select_ties<G, N, true>(key, l, k, mine, most);
+    if (my_expert >= 0) my_value = Key<T>::value(mine);
+    top = Key<T>::value(most);
+  } else if constexpr (sizeof(T) == 2) {
+    whole_keys();
+    const uint32_t mine = take_largest<G, N, K>(key, l, k, most, last, before);
+    if (mine > Key<T>::kMasked) {
+      my_expert = Key<T>::expert(mine);
+      my_value = Key<T>::value(mine);
+    }
+    top = Key<T>::value(most);
+  } else {
+    constexpr uint32_t kNumber = G * N - 1;                        // bits of an expert's number
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t e = (uint32_t)L::index(l, i);
+      key[i] = (int)e < n_experts ? (Key<T>::of(z[i], 0) & ~kNumber) | (kNumber - e) : 0u;
+    }
+    const uint32_t mine = take_largest<G, N, K + 1>(key, l, k + 1, most, last, before);
+    const bool valid = l < k && mine > Key<T>::kMasked;
+    if (valid) {
+      my_expert = (int)(kNumber - (mine & kNumber));
+      my_value = row[my_expert];
+    }
+    const uint32_t whole = Key<T>::of(my_value, 0);
+    const uint32_t next = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)mine, 0x101, 0xf, 0xf, true);        // row_shl:1
+    const uint32_t next_whole = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)whole, 0x101, 0xf, 0xf, true);
+    bool unclear = valid && l + 1 < k && ((mine ^ next) & ~kNumber) == 0 && whole != next_whole;
+    const bool border = before > Key<T>::kMasked && ((before ^ last) & ~kNumber) == 0;
+    if (__ballot(border)) {                                        // clear where all that agree in part agree in the whole
+      const uint32_t at = (uint32_t)__shfl((int)whole, (lane_index() & ~(G - 1)) + k - 1);
+#pragma unroll
+      for (int i = 0; i < N; ++i) unclear |= border && (Key<T>::of(z[i], 0) ^ at) - 1 < kNumber;
+    }
+    if (__ballot(unclear)) {
+      uint32_t key_of_mine;
+      whole_keys();
+      my_expert = select_ties<G, N, false>(key, l, k, key_of_mine, most);
+      my_value = my_expert >= 0 ? Key<T>::value(key_of_mine) : -INFINITY;
+    }
+    top = __uint_as_float(group_read<G, 0>(__float_as_uint(my_value)));
+  }
+}
+
+template <typename T, int G, int N, int K>
 __global__ void __launch_bounds__(kThreads) route_kernel(const T *logits, int64_t n_tokens, int n_experts, int64_t stride,
                                                          int k, int renorm, int32_t *experts, float *weights) {
-  using L = Layout<G, N>;
   const int l = (int)(threadIdx.x % G);
   const int64_t token = (int64_t)blockIdx.x * (kThreads / G) + threadIdx.x / G;
   const bool live = token < n_tokens;
-  float z[N];
-  load_row<T, G, N>(logits + (live ? token : 0) * stride, l, n_experts, z);
-  uint32_t key[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) key[i] = L::index(l, i) < n_experts ? Key<T>::of(z[i], L::index(l, i)) : 0u;
-  uint32_t my_key, top;
+  const T *row = logits + (live ? token : 0) * stride;
+  float z[N], my_value, m;
+  load_row<T, G, N>(row, l, n_experts, z);
   int my_expert;
-  select<T, G, N>(key, l, k, my_key, my_expert, top);
-  const float m = Key<T>::value(top);
-  const float mine = my_expert >= 0 ? exp_of(Key<T>::value(my_key) - m) : 0.0f;
+  select<T, G, N, K>(row, z, l, n_experts, k, my_expert, my_value, m);
+  const float mine = my_expert >= 0 ? exp_of(my_value - m) : 0.0f;
   float total;
   if (renorm) {
     total = group_sum<G>(mine);
@@ -198,13 +312,6 @@ __global__ void __launch_bounds__(kThreads) route_kernel(const T *logits, int64_
     experts[token * k + l] = my_expert;
     weights[token * k + l] = my_expert >= 0 ? mine / total : 0.0f;
   }
-}
-
-// Lane J's value of each group, for all its lanes.
-template <int G, int J>
-__device__ __forceinline__ uint32_t group_read(uint32_t x) {
-  if (G == 64) return (uint32_t)__builtin_amdgcn_readlane((int)x, J);
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + J, 0xf, 0xf, false);       // row_newbcast
 }
 
 // Sum of v over the lanes j < k of a group with this lane's e, in their order.
@@ -343,7 +450,10 @@ bfs_status bfs_moe_route(const void *logits, int32_t dtype, int64_t n_tokens, in
       if (!logits || !experts || !weights) return fail(BFS_E_INVALID, "moe_route: null buffer");
       return with_layout(n_experts, [&](auto g, auto n) {
         constexpr int G = decltype(g)::value, N = decltype(n)::value, kRows = kThreads / G;
-        return launch("moe_route", route_kernel<T, G, N>, (n_tokens + kRows - 1) / kRows, kThreads, 0, stream,
+        auto kernel = route_kernel<T, G, N, 2>;
+        if constexpr (kSorts<T, N, kMaxK>)
+          if (k > 2) kernel = k <= 8 ? route_kernel<T, G, N, 8> : route_kernel<T, G, N, kMaxK>;
+        return launch("moe_route", kernel, (n_tokens + kRows - 1) / kRows, kThreads, 0, stream,
                       static_cast<const T *>(logits), n_tokens, n_experts, logits_stride, k,
                       (int)(flags & BFS_MOE_RENORMALIZE), experts, weights);
       });

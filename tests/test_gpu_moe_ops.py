@@ -136,10 +136,42 @@ def test_route_ties_and_masks(e, dtype):
         assert (weights[experts < 0] == 0).all() and (experts[36] == -1).all()
 
 
-def test_route_nan_and_inf():
+@pytest.mark.parametrize("t,e,k", [(40, 65, 3), (64, 128, 8), (33, 256, 4), (50, 256, 16), (21, 300, 8), (13, 512, 16), (9, 1024, 5),
+                                   (16, 100, 16), (40, 64, 8)])
+@pytest.mark.parametrize("kind", ["steps", "ties", "few", "bf16", "masked"])
+def test_route_close_logits(t, e, k, kind):
+    """fp32 logits that differ in their last bits, or not at all, among the
+    chosen ones and at their border, in some rows or in all."""
+    g = torch.Generator().manual_seed(e * k)
+    z = torch.randn((t, e), generator=g) * 3.0
+    step = torch.randint(0, 6, (t, e), generator=g, dtype=torch.int32)
+    if kind == "steps":                                # all within a few steps of one value, of either sign
+        z = (torch.full((t, e), 1.5).view(torch.int32) + step).view(torch.float32) * torch.where(torch.arange(t) % 2 == 0, 1.0, -1.0)[:, None]
+    elif kind == "ties":                               # large ones all equal, more or fewer than k
+        z = torch.where(torch.rand((t, e), generator=g) < torch.rand((t, 1), generator=g) * 2 * k / e, torch.tensor(9.25), z)
+    elif kind == "few":                                # every seventh row has three near-equal largest ones, out of order
+        i = torch.arange(0, t, 7)
+        for n, (c, d) in enumerate(((e - 1, 2), (e // 2, 1), (0, 3))):
+            z[i, c] = (torch.tensor([11.0]).view(torch.int32) + d).view(torch.float32)
+    elif kind == "bf16":
+        z = z.bfloat16().float()
+    else:
+        z = torch.where(torch.rand((t, e), generator=g) < 0.97, torch.tensor(float("-inf")), z)
+        z[::3] = torch.where(step[::3] > 2, torch.tensor(torch.finfo(torch.float32).min), torch.tensor(-float("inf")))
+    z = z.cuda()
+    for renorm in (True, False):
+        experts, weights = bfsp.moe_route(z, k, renormalize=renorm)
+        ref_e, ref_w, arg = _route_reference(_f64(z), k, renorm)
+        assert np.array_equal(experts.cpu().numpy(), ref_e)
+        arg = np.where(ref_e < 0, 0.0, arg)
+        _close(weights, ref_w, 2 * (np.abs(arg) + e / 16 + 20) * U * ref_w)
+
+
+@pytest.mark.parametrize("e", [64, 256, 600])
+def test_route_nan_and_inf(e):
     """NaN ranks above everything and makes its token's weights NaN; +inf
     does so too; other tokens are not touched by it."""
-    z = _normal(1, (8, 64))
+    z = _normal(1, (8, e))
     clean = bfsp.moe_route(z, 4)
     z[2, 7] = float("nan")
     z[3, 9] = -float("nan")
