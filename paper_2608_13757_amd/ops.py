@@ -5,12 +5,14 @@ norm with clipping.
 Argument checks and marshalling only.  Tensors are torch tensors on the
 current device; a refused argument raises BfsError (E_INVALID or E_RESOURCE)
 before anything is launched.  An output must not share memory with an input or
-another output, except where it is said.  Outputs that are not given are allocated on the
-current stream.  ``stream``: a torch stream or handle, None the current one;
-on another stream than the current one every output (and the workspace) has to
-be given, since an allocation belongs to the stream that it was made on.
+another output, except where it is said.  Outputs that are not given are
+allocated on the current stream.  ``stream``: a torch stream or handle, None
+the current one; on another stream than the current one every output (and the
+workspace) has to be given, since an allocation belongs to the stream that it
+was made on.  No autograd graph is recorded: the gradients are calls of their
+own.
 
-Calls of a few tokens are bound by the host (2.9 us of a call are the launch),
+Calls of a few tokens are bound by the host (some 2.5 us of a call are the launch),
 so the checks stand in the calls themselves; the functions they call say what
 is wrong.
 """

@@ -76,6 +76,33 @@ def test_norm_and_clip(sizes, dtypes, max_norm):
     assert torch.equal(norm, norm2) and all(torch.equal(o, g) for o, g in zip(outs, grads))
 
 
+def test_thousands_of_tensors():
+    """More chunks than the launches of most sets have workgroups for."""
+    g = torch.Generator().manual_seed(10)
+    flat_in = (torch.randn(63000, generator=g) * 0.01).bfloat16().cuda()
+    sizes = [1 + i % 5 for i in range(21000)]
+    grads = list(flat_in.split(sizes))
+    ref = _check_norm(GradSet(grads).norm(), [flat_in])
+    out = torch.full((63000,), 5.0, device="cuda")
+    _check_norm(GradSet(grads, out=out).clip(0.25), [flat_in])
+    _check_out(out, flat_in, 0.25 / (ref + 1e-6), torch.float32)
+    assert GradSet(grads).clip(0.25) > 0                      # in place
+    _check_out(flat_in.float(), out, 1.0, torch.bfloat16)
+
+
+@pytest.mark.parametrize("dtype,n", [(torch.bfloat16, 2 ** 27 + 12345), (torch.float32, 2 ** 27)])
+def test_more_than_the_last_level_cache(dtype, n):
+    g = torch.Generator(device="cuda").manual_seed(11)
+    flat_in = torch.empty(n, dtype=dtype, device="cuda").normal_(0, 0.01, generator=g)
+    grads = list(flat_in.split([n // 2 + 1, 77, n - n // 2 - 78]))
+    ref = float(sum(x.double().square().sum() for x in grads)) ** 0.5
+    out = torch.empty(n, device="cuda")
+    for norm in (GradSet(grads).norm(), GradSet(grads, out=out).clip(1.0)):
+        assert abs(float(norm) - ref) <= ref * (U + n * 2.0 ** -52) * 1.001
+    want = flat_in.double().mul_(1.0 / (ref + 1e-6))
+    assert bool(((out.double() - want).abs() <= want.abs() * 4 * U).all())
+
+
 def test_same_bits_every_run_and_one_shot_calls():
     grads = _grads(3, [100003, 5000, 77], DTYPES, 1.0)
     s = GradSet(grads)

@@ -470,6 +470,43 @@ def test_combine_extremes(dtype):
     assert torch.isfinite(y).all() and (y[0] == 2).all()
 
 
+@pytest.mark.parametrize("t,k,e", [(3_000_001, 2, 5), (2_500_000, 1, 300)])
+def test_dispatch_of_many_tokens(t, k, e):
+    """Thousands of groups of slots, whose counts a launch of their own sums;
+    a narrow row for each."""
+    g = torch.Generator(device="cuda").manual_seed(e)
+    experts = torch.randint(-1, e, (t, k), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.arange(t, device="cuda", dtype=torch.float32)[:, None]
+    perm, off, pos, rows = bfsp.moe_dispatch(experts, e, x)
+    flat = experts.reshape(-1)
+    key, order = torch.sort(torch.where(flat < 0, e, flat), stable=True)
+    n = int((key < e).sum())
+    assert torch.equal(off.long(), torch.searchsorted(key, torch.arange(e + 1, device="cuda", dtype=torch.int32)))
+    assert torch.equal(perm[:n].long(), order[:n] // k) and torch.equal(rows[:n, 0], x[order[:n] // k, 0])
+    want = torch.full((t * k,), -1, dtype=torch.int32, device="cuda")
+    want[order[:n]] = torch.arange(n, device="cuda", dtype=torch.int32)
+    assert torch.equal(pos.reshape(-1), want)
+    z = torch.randn((t, 8), generator=g, device="cuda")
+    ids, w = bfsp.moe_route(z, 1, renormalize=False)
+    assert torch.equal(ids[:, 0].long(), z.argmax(1)) and torch.allclose(w, torch.softmax(z, 1).amax(1, keepdim=True), rtol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_no_width_and_no_tokens(dtype):
+    for t, h in ((5, 0), (0, 7), (0, 0), (1500, 0)):
+        experts = _experts(1, t, 2, 4)
+        x = torch.empty((t, h), dtype=dtype, device="cuda")
+        perm, off, pos, rows = bfsp.moe_dispatch(experts, 4, x)
+        assert rows.shape == (2 * t, h) and int(off[-1]) == 2 * t and pos.shape == (t, 2)
+        w = torch.ones((t, 2), device="cuda")
+        assert bfsp.moe_combine(rows, pos, w).shape == (t, h) and bfsp.moe_dispatch_grad(rows, pos).shape == (t, h)
+        drows, dw = bfsp.moe_combine_grad(x, rows, pos, w)
+        assert drows.shape == (2 * t, h) and dw.shape == (t, 2) and (dw == 0).all()
+    z = torch.empty((0, 12), dtype=dtype, device="cuda")
+    ids, w = bfsp.moe_route(z, 3)
+    assert ids.shape == (0, 3) and bfsp.moe_route_grad(z, ids, w).shape == (0, 12)
+
+
 def test_no_rows_at_all():
     pos = torch.zeros((3, 2), dtype=torch.int32, device="cuda")
     rows, w = torch.empty((0, 16), device="cuda"), torch.ones((3, 2), device="cuda")

@@ -2,6 +2,8 @@
 use them: router, dispatch, the MoE plans' products, combination; the
 gradients back to logits and tokens; clipping into the AdamW plan's flat
 gradient.  And as captured graphs, and on other streams."""
+import threading
+
 import numpy as np
 import pytest
 
@@ -221,3 +223,32 @@ def test_two_streams_at_once():
     gs.clip(1.0, norm=out[12], workspace=gw, stream=st)
     st.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(out, want[0]))
+
+
+def test_two_threads_at_once():
+    """Two host threads, each with its own stream and buffers; the set of
+    gradients is shared, its calls read it only."""
+    steps = [_Step(1200, 32, 4, 192, torch.bfloat16, seed=9 * i) for i in range(2)]
+    for i, s in enumerate(steps):
+        s.refill(i + 3)
+    shared = GradSet(steps[0].grads)
+    want = [s.run() + [shared.norm()] for s in steps]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got[i] = steps[i].run() + [shared.norm()]
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:          # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for a, b in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
