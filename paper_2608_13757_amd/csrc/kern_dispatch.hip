@@ -40,7 +40,9 @@ constexpr int kBlocks = 1024;                          // workgroups that rank a
 // 1024 bf16 to two experts of 64: 6.7 us, with a launch that counts 8.4; 8000
 // slots: 15.8 and 12.6)
 constexpr int kAlone = 4096;
-constexpr int64_t kSumEntries = 8192;                  // counts that every workgroup sums by itself
+// Counts that every ranking workgroup sums by itself (8000 tokens to eight of 128
+// experts, 8064 counts: 24.7 us, with a launch that sums them 23.4).
+constexpr int64_t kSumEntries = 4096;
 
 struct DispatchParams {
   const int32_t *experts;
