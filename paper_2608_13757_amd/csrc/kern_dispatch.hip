@@ -24,7 +24,7 @@
 // stores under way.
 //
 // Bound by memory: 32768 tokens of 4096 bf16 to two experts of 64 each, 806 MB,
-// in 156 us (5.2 TB/s, a large copy's rate), some 8 us of them the ranking.
+// in 154 us (5.2 TB/s, a large copy's rate), some 9 us of them the ranking.
 #include "op_common.h"
 
 using namespace bfsop;
@@ -273,6 +273,39 @@ __device__ __forceinline__ void copy_row(const DispatchParams &P, int64_t t, int
   }
 }
 
+// The same for rows of a line or more that follow each other without a gap and
+// begin anywhere in a line.  A row's lines are those that begin in it: the last
+// one ends with the next row's first elements, which are read from that row's
+// token.  So every line is written whole and once, where two waves on different
+// XCDs would write a part each.
+template <typename T>
+__device__ __forceinline__ void copy_row_lines(const DispatchParams &P, int64_t t, int64_t at, int64_t step, int slot) {
+  constexpr int E = Chunk<T>::kElems, kLineElems = kLine / (int)sizeof(T);
+  const T *x = static_cast<const T *>(P.x) + t * P.x_stride;
+  int next = -1;                                   // lane j: the token of the row behind slot j's
+  if (slot >= 0 && slot + 1 < P.off[P.n_experts]) next = P.perm[slot + 1];
+  for (uint64_t left = __ballot(slot >= 0); left; left &= left - 1) {
+    const int j = __builtin_ctzll(left), r = __builtin_amdgcn_readlane(slot, j), behind = __builtin_amdgcn_readlane(next, j);
+    T *row = static_cast<T *>(P.rows) + r * P.width;
+    const int64_t head = head_of(row, P.width), lines = (P.width - head) / kLineElems;
+    const int64_t i = head + lines * kLineElems + at, chunks = lines * (kLineElems / E);
+    const bool ends = at < kLineElems && i < P.width, starts = at < kLineElems && i >= P.width && behind >= 0;
+    T last = zero_of<T>();                         // this lane's element of the row's last line
+    if (ends) last = x[i];
+    if (starts) last = static_cast<const T *>(P.x)[behind * P.x_stride + (i - P.width)];
+    each_chunk<4>(at, chunks, step, [&](auto us, int64_t c) {
+      constexpr int U = decltype(us)::value;
+      typename Chunk<T>::vec v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = load<false>(x + head + (c + u * step) * E);
+#pragma unroll
+      for (int u = 0; u < U; ++u) store<true>(row + head + (c + u * step) * E, v[u]);
+    });
+    if (ends || (starts && i - at < P.width)) __builtin_nontemporal_store(last, row + i);
+    if (r == 0 && at < head) row[at] = x[at];      // before the first line
+  }
+}
+
 template <typename T, bool kStream>
 __global__ void __launch_bounds__(kThreads) dispatch_kernel(DispatchParams P) {
   extern __shared__ uint32_t lds[];
@@ -318,12 +351,15 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(DispatchParams P) {
 }
 
 // A wave takes a token, or one of `spans` parts of its row.
-template <typename T, bool kStream>
+template <typename T, bool kStream, bool kLines>
 __global__ void __launch_bounds__(kThreads) copy_kernel(DispatchParams P) {
   const int64_t u = (int64_t)blockIdx.x * kWaves + wave_index(), t = u / P.spans;
   if (t >= P.n_slots / P.k) return;
   const int lane = lane_index();
-  copy_row<T, kStream>(P, t, (u - t * P.spans) * kWave + lane, P.spans * kWave, lane < P.k ? P.pos[t * P.k + lane] : -1);
+  const int64_t at = (u - t * P.spans) * kWave + lane, step = P.spans * kWave;
+  const int slot = lane < P.k ? P.pos[t * P.k + lane] : -1;
+  if (kLines) copy_row_lines<T>(P, t, at, step, slot);
+  else copy_row<T, kStream>(P, t, at, step, slot);
 }
 
 __global__ void __launch_bounds__(kThreads) count_kernel(DispatchParams P) {
@@ -435,8 +471,7 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       const size_t lds = ((kWaves + 3) * (size_t)n_experts + 1 + kGroupSlots) * sizeof(uint32_t);
       const int64_t all = groups > 0 ? groups : 1;
       if (!P.x) return launch("moe_dispatch", dispatch_kernel<T, false>, all, kThreads, lds, stream, P);
-      // two waves for a row of four steps and more (32768 tokens of 4096 bf16 to
-      // two experts each: 156 us, with one 162), one step for each wave where the
+      // two waves for a row of four steps and more, one step for each wave where the
       // tokens are fewer than 512
       const int64_t steps = (width + kWave * Chunk<T>::kElems - 1) / (kWave * Chunk<T>::kElems);
       const int64_t wanted = (511 + n_tokens) / n_tokens, least = steps >= 4 ? 2 : 1;
@@ -452,7 +487,19 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       s = launch("moe_dispatch", dispatch_kernel<T, false>, all, kThreads, lds, stream, P);
       P.x = x;
       if (s != BFS_OK) return s;
-      return launch("moe_dispatch", stream_rows ? copy_kernel<T, true> : copy_kernel<T, false>,
+      // What passes the caches: rows in whole lines where those are shared
+      // (32768 tokens of 1409 bf16 to eight: 235 -> 197 us, 5003 to two: 240 ->
+      // 198), up to four waves for each; else a wave for each step of a row
+      // (4096 to one: 109 -> 100 us, 8192 to two 326 -> 315, 4096 to four 273 and
+      // 284), as far as the launch's size goes.
+      const int64_t bytes = width * (int64_t)sizeof(T);
+      const bool lines = stream_rows && rows_stride == width && bytes >= kLine && ((uintptr_t)rows % kLine || bytes % kLine);
+      if (stream_rows && steps >= 4) {
+        const int64_t most = (((int64_t)1 << 26) - kWaves) / n_tokens, each = lines ? steps >= 8 ? 4 : 2 : steps;
+        P.spans = each < most ? each : most;
+      }
+      return launch("moe_dispatch", !stream_rows ? copy_kernel<T, false, false> : lines ? copy_kernel<T, true, true>
+                                                                                       : copy_kernel<T, true, false>,
                     (n_tokens * P.spans + kWaves - 1) / kWaves, kThreads, 0, stream, P);
     };
     // rows are moved, not computed with: the element's size decides

@@ -91,6 +91,15 @@ __device__ __forceinline__ void store(T *p, typename Chunk<T>::vec v) {
   else *q = v;
 }
 
+constexpr int kLine = 128;                        // bytes of a cache line
+
+// Elements before the first whole line at p.
+template <typename T>
+__device__ __forceinline__ int head_of(const T *p, int64_t n) {
+  const int h = (int)((kLine - (uintptr_t)p % kLine) % kLine / sizeof(T));
+  return h < n ? h : (int)n;
+}
+
 // Waves that share a token's row of `most` steps of a wave: one round of four
 // steps for each (32768 tokens, 2 rows of 4096 bf16 combined: 129 us, with one
 // wave for all eight steps 138), one step where that leaves the compute units

@@ -470,6 +470,31 @@ def test_combine_extremes(dtype):
     assert torch.isfinite(y).all() and (y[0] == 2).all()
 
 
+@pytest.mark.parametrize("t,k,e,h,dtype,shift,drop", [
+    (9001, 3, 40, 1409, torch.float16, 0, 0.0), (9001, 3, 40, 1409, torch.float16, 3, 0.1), (300_001, 2, 7, 65, torch.bfloat16, 1, 0.3),
+    (4000, 8, 64, 1027, torch.float32, 5, 0.2), (260_000, 2, 9, 33, torch.float32, 0, 0.5), (6001, 2, 3, 4098, torch.bfloat16, 0, 0.0),
+    (500_000, 1, 4, 64, torch.bfloat16, 7, 0.1), (400_000, 1, 4, 63, torch.bfloat16, 0, 0.1), (20_000, 2, 4, 1024, torch.bfloat16, 32, 0.9),
+    (9001, 3, 40, 1409, torch.bfloat16, 1, 1.0)])
+def test_dispatch_past_the_caches(t, k, e, h, dtype, shift, drop):
+    """Calls whose rows are not kept in the caches: rows that share lines, from
+    an aligned address or not, rows of a line and less, many slots dropped.
+    What lies before the rows, and behind the last one, is left as it was."""
+    assert (k + 1) * t * h * dtype.itemsize > 96 << 20 or h < 64
+    experts = _experts(t, t, k, e, drop=drop)
+    x = _normal(h, (1 << 12, h), dtype)[torch.arange(t, device="cuda") * 7919 % (1 << 12)]
+    x[:, 0] = torch.arange(t, device="cuda") % 1021
+    x[:, -1] = torch.arange(t, device="cuda") // 1021
+    buf = torch.full((t * k * h + 64 + shift,), 77, dtype=dtype, device="cuda")
+    rows = buf[shift:shift + t * k * h].view(t * k, h)
+    perm, off, pos, _ = bfsp.moe_dispatch(experts, e, x, rows=rows)
+    n = int(off[-1])
+    assert n == int((experts >= 0).sum())
+    assert torch.equal(rows[:n], x[perm[:n].long()])
+    assert (buf[:shift] == 77).all() and (buf[shift + n * h:] == 77).all()
+    ref = bfsp.moe_dispatch(experts, e)
+    assert torch.equal(ref[0][:n], perm[:n]) and torch.equal(ref[2], pos)
+
+
 @pytest.mark.parametrize("t,k,e", [(3_000_001, 2, 5), (2_500_000, 1, 300)])
 def test_dispatch_of_many_tokens(t, k, e):
     """Thousands of groups of slots, whose counts a launch of their own sums;
