@@ -29,6 +29,11 @@ namespace {
 
 constexpr int kThreads = 256, kBlockWaves = kThreads / kWave;
 constexpr int kMaxK = 64;
+// Bytes of a row from which the gradient's rows that begin anywhere in a line
+// are written by lines (32768 tokens, eight rows of 1409 bf16: 383 -> 332 us,
+// two of 5003: 353 -> 316; 16000 tokens, four rows of 1201: 88 and 88, of 1001:
+// 65 and 74, as the lines' ends are a larger part).
+constexpr int64_t kLinesFrom = 2304;
 
 struct CombineParams {
   const void *rows, *dy;
@@ -182,8 +187,71 @@ __device__ __forceinline__ void grad_slots(const CombineParams &P, const T *dy, 
   }
 }
 
+// The same where the gradient's rows begin anywhere in a line: its whole lines,
+// and the elements before and behind them one by one.
+template <typename T, int N>
+__device__ __forceinline__ void grad_slots_lines(const CombineParams &P, const T *dy, const int64_t *p, const float *w, int64_t at,
+                                                 int64_t step, float (&dot)[N]) {
+  constexpr int E = Chunk<T>::kElems, kMost = N == 4 ? 2 : 4;
+  typedef typename Chunk<T>::vec vec;
+  const T *row[N];
+  T *out[N];
+  int64_t head[N], chunks[N], least = P.width;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    row[n] = static_cast<const T *>(P.rows) + p[n] * P.rows_stride;
+    out[n] = static_cast<T *>(P.out) + p[n] * P.out_stride;
+    head[n] = head_of(out[n], P.width);
+    chunks[n] = (P.width - head[n]) * (int64_t)sizeof(T) / kLine * (kLine / 16);
+    least = chunks[n] < least ? chunks[n] : least;
+    dot[n] = 0.0f;
+  }
+  auto take = [&](int n, int64_t i, vec g, vec v) {
+    vec o;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      dot[n] += (float)g[e] * (float)v[e];
+      o[e] = (T)(w[n] * (float)g[e]);
+    }
+    store<true>(out[n] + i, o);
+  };
+  each_chunk<kMost>(at, least, step, [&](auto us, int64_t c) {
+    constexpr int U = decltype(us)::value;
+    vec g[N][U], v[N][U];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = head[n] + (c + u * step) * E;
+        g[n][u] = *reinterpret_cast<const vec *>(dy + i);
+        v[n][u] = load<true>(row[n] + i);
+      }
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int u = 0; u < U; ++u) take(n, head[n] + (c + u * step) * E, g[n][u], v[n][u]);
+  });
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    // one line's difference between the rows, then the ends
+    const int64_t c = least + at;
+    if (c < chunks[n]) {
+      const int64_t i = head[n] + c * E;
+      take(n, i, *reinterpret_cast<const vec *>(dy + i), load<true>(row[n] + i));
+    }
+    auto one = [&](int64_t i) {
+      const float g = (float)dy[i];
+      dot[n] += g * (float)row[n][i];
+      out[n][i] = (T)(w[n] * g);
+    };
+    if (at < head[n]) one(at);
+    const int64_t i = head[n] + chunks[n] * E + at;
+    if (at < kWave && i < P.width) one(i);
+  }
+}
+
 // W waves take a token.
-template <typename T, int W, bool kStream>
+template <typename T, int W, bool kStream, bool kLines>
 __global__ void __launch_bounds__(kThreads) combine_grad_kernel(CombineParams P) {
   __shared__ float part[W > 1 ? W : 1][kMaxK];
   const int64_t t = ((int64_t)blockIdx.x * kBlockWaves + wave_index()) / W;
@@ -201,7 +269,9 @@ __global__ void __launch_bounds__(kThreads) combine_grad_kernel(CombineParams P)
       p[n] = __builtin_amdgcn_readlane(slot, j[n]);
       w[n] = readlane(weight, j[n]);
     }
-    grad_slots<T, N, kStream>(P, static_cast<const T *>(P.dy) + t * P.dy_stride, p, w, wave * kWave + lane, W * kWave, dot);
+    const T *dy = static_cast<const T *>(P.dy) + t * P.dy_stride;
+    if (kLines) grad_slots_lines<T, N>(P, dy, p, w, wave * kWave + lane, W * kWave, dot);
+    else grad_slots<T, N, kStream>(P, dy, p, w, wave * kWave + lane, W * kWave, dot);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const float d = group_sum<64>(dot[n]);
@@ -296,12 +366,15 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
       P.out_stride = grad_rows_stride;
       P.k = k;
       const bool stream_rows = (2 * k + 1) * n_tokens * width * (int64_t)sizeof(T) >= kStreamFrom;
-      if (width / Chunk<T>::kElems >= kThreads)
-        return launch("moe_combine_grad",
-                      stream_rows ? combine_grad_kernel<T, kBlockWaves, true> : combine_grad_kernel<T, kBlockWaves, false>,
-                      n_tokens, kThreads, 0, stream, P);
-      return launch("moe_combine_grad", stream_rows ? combine_grad_kernel<T, 1, true> : combine_grad_kernel<T, 1, false>,
-                    (n_tokens + kBlockWaves - 1) / kBlockWaves, kThreads, 0, stream, P);
+      const bool lines = stream_rows && width * (int64_t)sizeof(T) >= kLinesFrom &&
+                         ((uintptr_t)grad_rows % kLine || grad_rows_stride * sizeof(T) % kLine);
+      auto run = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        return launch("moe_combine_grad", !stream_rows ? combine_grad_kernel<T, W, false, false>
+                                          : lines ? combine_grad_kernel<T, W, true, true> : combine_grad_kernel<T, W, true, false>,
+                      W > 1 ? n_tokens : (n_tokens + kBlockWaves - 1) / kBlockWaves, kThreads, 0, stream, P);
+      };
+      return width / Chunk<T>::kElems >= kThreads ? run(Int<kBlockWaves>{}) : run(Int<1>{});
     });
   });
 }

@@ -495,6 +495,30 @@ def test_dispatch_past_the_caches(t, k, e, h, dtype, shift, drop):
     assert torch.equal(ref[0][:n], perm[:n]) and torch.equal(ref[2], pos)
 
 
+@pytest.mark.parametrize("t,k,h,dtype,shift", [
+    (6001, 3, 1409, torch.float16, 0), (6001, 3, 1409, torch.bfloat16, 3), (3000, 5, 1153, torch.float32, 7), (9000, 1, 2500, torch.float16, 1),
+    (2001, 2, 5003, torch.float32, 2), (4001, 2, 4104, torch.bfloat16, 0), (5000, 7, 1152, torch.bfloat16, 5), (1001, 16, 2047, torch.float16, 0)])
+def test_combine_grad_past_the_caches(t, k, h, dtype, shift):
+    """Rows of the gradient that begin anywhere in a line, some of them
+    dropped; what lies before them and behind the last one stays."""
+    assert (2 * k + 1) * t * h * dtype.itemsize >= 96 << 20
+    pos = bfsp.moe_dispatch(_experts(t, t, k, 9, drop=0.15), 9)[2]
+    n = int(pos.max()) + 1
+    rows, dy, w = _normal(h, (t * k, h), dtype), _normal(h + 1, (t, h), dtype), _normal(k, (t, k))
+    buf = torch.full((t * k * h + 64 + shift,), 77, dtype=dtype, device="cuda")
+    out, dw = bfsp.moe_combine_grad(dy, rows, pos, w, grad_rows=buf[shift:shift + t * k * h].view(t * k, h))
+    ok = pos >= 0
+    at, token = pos[ok].long(), torch.arange(t, device="cuda")[:, None].expand(t, k)[ok]
+    # a product rounded to fp32 and then to the type, or (one instruction does both for fp16) to the type at once
+    fi, ref = torch.finfo(dtype), w[ok][:, None].double() * dy[token].double()
+    assert bool(((out[at].double() - ref).abs() <= ref.abs() * (U + fi.eps / 2 * (1 + U)) + fi.tiny * fi.eps / 2).all())
+    assert (buf[:shift] == 77).all() and (buf[shift + n * h:] == 77).all() and (dw[~ok] == 0).all()
+    for j in range(k):
+        m = ok[:, j]
+        prod = dy[m].double() * rows[pos[m, j].long()].double()
+        assert bool(((dw[m, j].double() - prod.sum(1)).abs() <= (h / 64 + 16) * U * prod.abs().sum(1)).all())
+
+
 @pytest.mark.parametrize("t,k,e", [(3_000_001, 2, 5), (2_500_000, 1, 300)])
 def test_dispatch_of_many_tokens(t, k, e):
     """Thousands of groups of slots, whose counts a launch of their own sums;
