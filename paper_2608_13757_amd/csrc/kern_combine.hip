@@ -141,6 +141,89 @@ __global__ void __launch_bounds__(kThreads) combine_kernel(CombineParams P) {
   }
 }
 
+// Slots j .. j + 3 of token t, for any lane: rows (-1 without one) and weights.
+__device__ __forceinline__ void load_slots(const CombineParams &P, int64_t t, int j, int (&p)[4], float (&w)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    p[i] = -1;
+    w[i] = 1.0f;
+    if (j + i < P.k) {
+      const int row = P.pos[t * P.k + j + i];
+      p[i] = row >= 0 && row < P.n_rows ? row : -1;
+      if (P.weights) w[i] = P.weights[t * P.k + j + i];
+    }
+  }
+}
+
+// Narrow rows: G lanes take a token, a chunk each.
+template <typename T, int G>
+__global__ void __launch_bounds__(kThreads) combine_narrow_kernel(CombineParams P) {
+  constexpr int E = Chunk<T>::kElems;
+  const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / G;
+  const int c = (int)threadIdx.x % G;
+  if (t >= P.n_tokens || c * E >= P.width) return;
+  float acc[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  for (int j = 0; j < P.k; j += 4) {
+    int p[4];
+    float w[4];
+    typename Chunk<T>::vec v[4];
+    load_slots(P, t, j, p, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (p[i] >= 0) v[i] = load_chunk(static_cast<const T *>(P.rows) + p[i] * P.rows_stride, c, P.width);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (p[i] < 0) continue;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += w[i] * (float)v[i][e];
+    }
+  }
+  typename Chunk<T>::vec o;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = (T)acc[e];
+  store_chunk(static_cast<T *>(P.out) + t * P.out_stride, c, P.width, o);
+}
+
+template <typename T, int G>
+__global__ void __launch_bounds__(kThreads) combine_grad_narrow_kernel(CombineParams P) {
+  constexpr int E = Chunk<T>::kElems;
+  typedef typename Chunk<T>::vec vec;
+  const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / G;
+  const int c = (int)threadIdx.x % G;
+  if (t >= P.n_tokens) return;
+  const bool has = c * E < P.width;
+  vec g;
+  if (has) g = load_chunk(static_cast<const T *>(P.dy) + t * P.dy_stride, c, P.width);
+  for (int j = 0; j < P.k; j += 4) {
+    int p[4];
+    float w[4];
+    vec v[4];
+    load_slots(P, t, j, p, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (has && p[i] >= 0) v[i] = load_chunk(static_cast<const T *>(P.rows) + p[i] * P.rows_stride, c, P.width);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (j + i >= P.k) break;
+      float dot = 0.0f;
+      if (has && p[i] >= 0) {
+        vec o;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          dot += (float)g[e] * (float)v[i][e];
+          o[e] = (T)(w[i] * (float)g[e]);
+        }
+        store_chunk(static_cast<T *>(P.out) + p[i] * P.out_stride, c, P.width, o);
+      }
+#pragma unroll
+      for (int d = G / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d);
+      if (c == 0) P.grad_weights[t * P.k + j + i] = dot;
+    }
+  }
+}
+
 // <dy, rows[p_n]> over this lane's part of the rows, and rows of w_n * dy; for
 // N slots.
 template <typename T, int N, bool kStream>
@@ -326,6 +409,12 @@ bfs_status bfs_moe_combine(const void *rows, int32_t dtype, int64_t n_rows, int6
       P.k = k;
       const int64_t chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
       const int64_t most = (chunks + kWave - 1) / kWave;
+      if (narrow_rows(chunks, n_tokens, k))
+        return with_group(chunks, [&](auto g) {
+          constexpr int G = decltype(g)::value;
+          return launch("moe_combine", combine_narrow_kernel<T, G>, (n_tokens + kThreads / G - 1) / (kThreads / G), kThreads, 0,
+                        stream, P);
+        });
       P.spans = (int32_t)spans_of(most, n_tokens);
       // chunks of a lane at once: four where a wave's part of the row has them
       auto kernel = most >= 4 * P.spans ? combine_kernel<T, 4, false> : combine_kernel<T, 2, false>;
@@ -365,6 +454,13 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
       P.dy_stride = grad_y_stride;
       P.out_stride = grad_rows_stride;
       P.k = k;
+      const int64_t chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
+      if (narrow_rows(chunks, n_tokens, k))
+        return with_group(chunks, [&](auto g) {
+          constexpr int G = decltype(g)::value;
+          return launch("moe_combine_grad", combine_grad_narrow_kernel<T, G>, (n_tokens + kThreads / G - 1) / (kThreads / G),
+                        kThreads, 0, stream, P);
+        });
       const bool stream_rows = (2 * k + 1) * n_tokens * width * (int64_t)sizeof(T) >= kStreamFrom;
       const bool lines = stream_rows && width * (int64_t)sizeof(T) >= kLinesFrom &&
                          ((uintptr_t)grad_rows % kLine || grad_rows_stride * sizeof(T) % kLine);

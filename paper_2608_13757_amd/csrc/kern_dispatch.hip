@@ -362,6 +362,23 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(DispatchParams P) {
   else copy_row<T, kStream>(P, t, at, step, slot);
 }
 
+// Narrow rows: G lanes take a token, a chunk each.
+template <typename T, int G>
+__global__ void __launch_bounds__(kThreads) copy_narrow_kernel(DispatchParams P) {
+  const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / G;
+  const int c = (int)threadIdx.x % G;
+  if (t >= P.n_slots / P.k || c * Chunk<T>::kElems >= P.width) return;
+  const auto v = load_chunk(static_cast<const T *>(P.x) + t * P.x_stride, c, P.width);
+  for (int j = 0; j < P.k; j += 4) {
+    int row[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row[i] = j + i < P.k ? P.pos[t * P.k + j + i] : -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row[i] >= 0) store_chunk(static_cast<T *>(P.rows) + row[i] * P.rows_stride, c, P.width, v);
+  }
+}
+
 __global__ void __launch_bounds__(kThreads) count_kernel(DispatchParams P) {
   extern __shared__ uint32_t lds[];
   const int wave = wave_index(), lane = lane_index();
@@ -487,6 +504,13 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       s = launch("moe_dispatch", dispatch_kernel<T, false>, all, kThreads, lds, stream, P);
       P.x = x;
       if (s != BFS_OK) return s;
+      const int64_t row_chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
+      if (narrow_rows(row_chunks, n_tokens, k))
+        return with_group(row_chunks, [&](auto g) {
+          constexpr int G = decltype(g)::value;
+          return launch("moe_dispatch", copy_narrow_kernel<T, G>, (n_tokens + kThreads / G - 1) / (kThreads / G), kThreads, 0,
+                        stream, P);
+        });
       // What passes the caches: rows in whole lines where those are shared
       // (32768 tokens of 1409 bf16 to eight: 235 -> 197 us, 5003 to two: 240 ->
       // 198), up to four waves for each; else a wave for each step of a row

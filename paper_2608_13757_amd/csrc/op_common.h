@@ -91,6 +91,23 @@ __device__ __forceinline__ void store(T *p, typename Chunk<T>::vec v) {
   else *q = v;
 }
 
+// Whether a group of lanes (8, 16 or 32, a chunk each) takes a token, where a
+// wave would leave most of its lanes idle (us with a wave and with a group: two
+// rows of 64 bf16 combined, 32768 tokens 10.8 and 3.8, 8000 3.9 and 2.6, 4000 3.1
+// and 2.6, their gradient 18.7 and 6.1, 5.2 and 3.5, 3.5 and 3.4; eight rows of
+// 256, 32768 tokens: 26.4 and 33.1, four 16.2 and 14.8).
+inline bool narrow_rows(int64_t chunks, int64_t n_tokens, int32_t k) {
+  return chunks <= (k <= 4 ? 32 : 16) && n_tokens >= 6144;
+}
+
+// f(lanes of a group) for rows of up to 32 chunks.
+template <typename F>
+bfs_status with_group(int64_t chunks, F f) {
+  if (chunks <= 8) return f(Int<8>{});
+  if (chunks <= 16) return f(Int<16>{});
+  return f(Int<32>{});
+}
+
 constexpr int kLine = 128;                        // bytes of a cache line
 
 // Elements before the first whole line at p.
