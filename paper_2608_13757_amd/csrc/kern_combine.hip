@@ -17,8 +17,10 @@
 // row; the gradient two, with dy's).  In the combination a wave takes a token's
 // row or a part of it (op_common.h: spans_of); in the gradient, whose dot
 // products join the whole row, a workgroup takes a token where its four waves
-// have a step each, else a wave does (32768 tokens, two rows of 4096 bf16: 246
-// us, with a wave for each token 256; one row of 1024: 76 and 35 us).
+// have two steps each, and with four rows and more one step, else a wave does
+// (16000 tokens of 4096 bf16, two rows: 120 us with a workgroup and 125 with a
+// wave for each, of 2048 57 and 53; seven rows of 2048: 183 and 191; of 2248,
+// which begin anywhere in a line: 306 and 210).
 // 16384 tokens of eight rows of 2048 bf16, 605 MB: 100 us (6.0 TB/s; a large
 // copy runs at 5.3), its gradient, 1.14 GB, 203 us (5.6).
 #include "op_common.h"
@@ -470,7 +472,8 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
                                           : lines ? combine_grad_kernel<T, W, true, true> : combine_grad_kernel<T, W, true, false>,
                       W > 1 ? n_tokens : (n_tokens + kBlockWaves - 1) / kBlockWaves, kThreads, 0, stream, P);
       };
-      return width / Chunk<T>::kElems >= kThreads ? run(Int<kBlockWaves>{}) : run(Int<1>{});
+      const int64_t whole = width / Chunk<T>::kElems;
+      return whole >= 2 * kThreads || (whole >= kThreads && k >= 4 && !lines) ? run(Int<kBlockWaves>{}) : run(Int<1>{});
     });
   });
 }

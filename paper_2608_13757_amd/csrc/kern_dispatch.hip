@@ -13,13 +13,13 @@
 // rows come in the same order in every run.  LDS atomics only count.
 //
 // The slots go in groups of up to 1024, a workgroup ranks a whole group.  Up to
-// 4096 slots it counts the other groups' too.  Beyond, one launch counts each
+// 8192 slots it counts the other groups' too.  Beyond, one launch counts each
 // group's slots by expert, and the ranking workgroups sum the groups before
 // theirs, or, where that table is long, read sums that one more launch makes.
-// The rows are copied by the ranking workgroups where 1024 of them give each
+// The rows are copied by the ranking workgroups where 512 of them give each
 // wave one part of a row: several then rank the same group, each for itself,
-// and one launch is saved (2048 tokens of 4096 bf16 to 8 experts each: 33.4 us,
-// with the copy in a launch of its own 35.6; 128 tokens to two: 5 us in a single
+// and one launch is saved (2048 tokens of 4096 bf16 to 8 experts each: 32 us,
+// with the copy in a launch of its own 35; 128 tokens to two: 3.9 us in a single
 // launch).  Beyond, the copy is a launch of its own, whose waves end with their
 // stores under way.
 //
@@ -32,14 +32,18 @@ using namespace bfsop;
 namespace {
 
 constexpr int kMaxExperts = 1024, kMaxK = 64;
-constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kBatches = 4;                            // batches of 64 slots per wave
+// Ranking: a group's batches of 64 slots over eight waves, two each (1000 tokens
+// to two of 64 experts 5.3 us, over four waves, four each, 6.3; 4000 to one 7.6
+// and 10.6; 8 tokens 3.9 and 3.7).
+constexpr int kWaves = 8, kThreads = kWaves * kWave;
+constexpr int kBatches = 2;
+constexpr int kCopyWaves = 4, kCopyThreads = kCopyWaves * kWave;
 constexpr int kGroupSlots = kWaves * kBatches * kWave;
-constexpr int kBlocks = 1024;                          // workgroups that rank and copy, at most
-// Slots up to which every ranking workgroup counts all by itself (1000 tokens of
-// 1024 bf16 to two experts of 64: 6.7 us, with a launch that counts 8.4; 8000
-// slots: 15.8 and 12.6)
-constexpr int kAlone = 4096;
+constexpr int kBlocks = 512;                          // workgroups that rank and copy, at most
+// Slots up to which every ranking workgroup counts all by itself (3000 tokens of
+// 512 bf16 to two experts of 64: 8.5 us, with a launch that counts 9.4; 16000 to
+// one of 16: 19.3 and 18.0).
+constexpr int kAlone = 8192;
 // Counts that every ranking workgroup sums by itself (8000 tokens to eight of 128
 // experts, 8064 counts: 24.7 us, with a launch that sums them 23.4).
 constexpr int64_t kSumEntries = 4096;
@@ -51,17 +55,23 @@ struct DispatchParams {
   void *rows;
   uint32_t *counts;              // [n_groups][n_experts]; with sums: of the groups before, and [n_groups]: of all
   int64_t n_slots, x_stride, rows_stride, width, spans;
-  int32_t k, n_experts, n_groups, group, parts, bits;   // group: slots of one, whole tokens
+  int32_t k, n_experts, n_groups, group, parts, bits, batches;   // group: slots of one, whole tokens
 };
 
-// The ids of this lane's slots of group g: wave w holds batches
-// w * kBatches ...; -1 without an expert or past the end.
+// The place in its group of this lane's slot of batch b: a wave's batches follow
+// each other, as many for each wave as a group needs (P.batches).
+__device__ __forceinline__ int place_of(const DispatchParams &P, int wave, int lane, int b) {
+  return (wave * P.batches + b) * kWave + lane;
+}
+
+// The ids of this lane's slots of group g; -1 without an expert, past the end and
+// in batches that are not used.
 __device__ __forceinline__ void load_ids(const DispatchParams &P, int g, int wave, int lane, int (&id)[kBatches]) {
 #pragma unroll
   for (int b = 0; b < kBatches; ++b) {
-    const int i = (wave * kBatches + b) * kWave + lane;
+    const int i = place_of(P, wave, lane, b);
     const int64_t s = (int64_t)g * P.group + i;
-    const int e = i < P.group && s < P.n_slots ? P.experts[s] : -1;
+    const int e = b < P.batches && i < P.group && s < P.n_slots ? P.experts[s] : -1;
     id[b] = (uint32_t)e < (uint32_t)P.n_experts ? e : -1;
   }
 }
@@ -141,12 +151,7 @@ __device__ __forceinline__ void expert_starts(int n_experts, const uint32_t *tot
     for (int e0 = 0; e0 < n_experts; e0 += kWave) {
       const int e = e0 + lane;
       const uint32_t c = e < n_experts ? total[e] : 0;
-      uint32_t sum = c;
-#pragma unroll
-      for (int d = 1; d < kWave; d <<= 1) {
-        const uint32_t up = (uint32_t)__shfl_up((int)sum, d);
-        sum += lane >= d ? up : 0;
-      }
+      const uint32_t sum = wave_scan(c);
       if (e < n_experts) start[e] = before + sum - c;
       before += (uint32_t)__builtin_amdgcn_readlane((int)sum, kWave - 1);
     }
@@ -191,7 +196,7 @@ __device__ __forceinline__ void rank_slots(const DispatchParams &P, const int (&
 // counts its own slots (8000 tokens to eight experts of 64: 23.4 -> 21.3 us; 2000
 // to four of 8, a table of 64 counts: 9.1 and 9.6).
 struct GroupSums {
-  static constexpr int kAhead = 16, kAheadFrom = 1024;
+  static constexpr int kAhead = 8, kAheadFrom = 1024;
   int share, my, e0;
   bool table, early;
   uint32_t ahead[kAhead];
@@ -331,7 +336,8 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(DispatchParams P) {
     for (int e = (int)threadIdx.x; e <= E; e += kThreads) P.off[e] = (int32_t)start[e];
 #pragma unroll
   for (int b = 0; b < kBatches; ++b) {
-    const int i = (wave * kBatches + b) * kWave + lane;
+    if (b >= P.batches) break;
+    const int i = place_of(P, wave, lane, b);
     rows[i] = row[b];
     if (part == 0 && i < P.group && first + i < P.n_slots) {
       P.pos[first + i] = row[b];
@@ -352,8 +358,8 @@ __global__ void __launch_bounds__(kThreads) dispatch_kernel(DispatchParams P) {
 
 // A wave takes a token, or one of `spans` parts of its row.
 template <typename T, bool kStream, bool kLines>
-__global__ void __launch_bounds__(kThreads) copy_kernel(DispatchParams P) {
-  const int64_t u = (int64_t)blockIdx.x * kWaves + wave_index(), t = u / P.spans;
+__global__ void __launch_bounds__(kCopyThreads) copy_kernel(DispatchParams P) {
+  const int64_t u = (int64_t)blockIdx.x * kCopyWaves + wave_index(), t = u / P.spans;
   if (t >= P.n_slots / P.k) return;
   const int lane = lane_index();
   const int64_t at = (u - t * P.spans) * kWave + lane, step = P.spans * kWave;
@@ -364,8 +370,8 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(DispatchParams P) {
 
 // Narrow rows: G lanes take a token, a chunk each.
 template <typename T, int G>
-__global__ void __launch_bounds__(kThreads) copy_narrow_kernel(DispatchParams P) {
-  const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / G;
+__global__ void __launch_bounds__(kCopyThreads) copy_narrow_kernel(DispatchParams P) {
+  const int64_t t = ((int64_t)blockIdx.x * kCopyThreads + threadIdx.x) / G;
   const int c = (int)threadIdx.x % G;
   if (t >= P.n_slots / P.k || c * Chunk<T>::kElems >= P.width) return;
   const auto v = load_chunk(static_cast<const T *>(P.x) + t * P.x_stride, c, P.width);
@@ -403,12 +409,7 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(DispatchParams P) {
     const int g = g0 + lane;
     uint32_t *at = P.counts + (int64_t)g * P.n_experts + e;
     const uint32_t c = g < P.n_groups ? *at : 0;
-    uint32_t sum = c;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const uint32_t up = (uint32_t)__shfl_up((int)sum, d);
-      sum += lane >= d ? up : 0;
-    }
+    const uint32_t sum = wave_scan(c);
     if (g < P.n_groups) *at = before + sum - c;
     before += (uint32_t)__builtin_amdgcn_readlane((int)sum, kWave - 1);
   }
@@ -477,6 +478,8 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
     P.n_groups = (int32_t)groups;
     P.group = group_of(k);
     P.parts = 1;
+    const int64_t in_first = slots < P.group ? slots : P.group;
+    P.batches = in_first > 0 ? (int32_t)((in_first + kThreads - 1) / kThreads) : 1;
     while ((1 << P.bits) < n_experts) ++P.bits;
     auto copy = [&](auto t) -> bfs_status {
       using T = decltype(t);
@@ -508,8 +511,8 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       if (narrow_rows(row_chunks, n_tokens, k))
         return with_group(row_chunks, [&](auto g) {
           constexpr int G = decltype(g)::value;
-          return launch("moe_dispatch", copy_narrow_kernel<T, G>, (n_tokens + kThreads / G - 1) / (kThreads / G), kThreads, 0,
-                        stream, P);
+          return launch("moe_dispatch", copy_narrow_kernel<T, G>, (n_tokens + kCopyThreads / G - 1) / (kCopyThreads / G),
+                        kCopyThreads, 0, stream, P);
         });
       // What passes the caches: rows in whole lines where those are shared
       // (32768 tokens of 1409 bf16 to eight: 235 -> 197 us, 5003 to two: 240 ->
@@ -519,12 +522,12 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       const int64_t bytes = width * (int64_t)sizeof(T);
       const bool lines = stream_rows && rows_stride == width && bytes >= kLine && ((uintptr_t)rows % kLine || bytes % kLine);
       if (stream_rows && steps >= 4) {
-        const int64_t most = (((int64_t)1 << 26) - kWaves) / n_tokens, each = lines ? steps >= 8 ? 4 : 2 : steps;
+        const int64_t most = (((int64_t)1 << 26) - kCopyWaves) / n_tokens, each = lines ? steps >= 8 ? 4 : 2 : steps;
         P.spans = each < most ? each : most;
       }
       return launch("moe_dispatch", !stream_rows ? copy_kernel<T, false, false> : lines ? copy_kernel<T, true, true>
                                                                                        : copy_kernel<T, true, false>,
-                    (n_tokens * P.spans + kWaves - 1) / kWaves, kThreads, 0, stream, P);
+                    (n_tokens * P.spans + kCopyWaves - 1) / kCopyWaves, kCopyThreads, 0, stream, P);
     };
     // rows are moved, not computed with: the element's size decides
     switch (dtype) {

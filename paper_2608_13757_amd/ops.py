@@ -29,7 +29,7 @@ from .bfs import E_INVALID, E_RESOURCE, OK, BfsError
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 MOE_RENORMALIZE = 1
 MAX_EXPERTS = 1024
-DISPATCH_ALONE = 4096            # slots up to which a dispatch needs no workspace
+DISPATCH_ALONE = 8192            # slots up to which a dispatch needs no workspace
 # bfs_call's words: the operator, the number of its arguments, the arguments
 _ROUTE, _ROUTE_GRAD, _DISPATCH, _COMBINE, _COMBINE_GRAD, _NORM, _CLIP = (
     struct.Struct(f).pack for f in ("12q", "14q", "18q", "14q", "17q", "8q", "4qd4q"))

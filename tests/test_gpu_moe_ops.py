@@ -287,10 +287,10 @@ def _dispatch_reference(experts, e):
     return slots // experts.shape[1], off, pos.reshape(experts.shape)
 
 
-# around one wave's batch, one group (1024 slots) and one launch's limit (4096)
+# around one wave's batch, one group (1024 slots) and one launch's limit (8192)
 DISPATCH = [(0, 2, 5, 8), (1, 1, 1, 1), (1, 8, 64, 4096), (3, 1, 5, 7), (8, 2, 64, 130), (63, 1, 3, 16), (65, 1, 1, 33),
             (128, 8, 64, 24), (1024, 1, 17, 8), (1025, 1, 17, 9), (512, 2, 1024, 12), (342, 3, 300, 65), (4096, 1, 64, 4),
-            (4097, 1, 64, 3), (1500, 7, 256, 40), (9001, 4, 33, 17), (7000, 2, 16, 40), (6500, 8, 8, 120), (6200, 3, 5, 250), (9001, 5, 7, 131), (6144, 16, 9, 1), (1365, 3, 90, 11), (1366, 3, 90, 11), (511, 5, 1024, 6), (585, 7, 2, 19), (2047, 2, 700, 5), (2, 64, 100, 20), (300, 64, 1000, 8)]
+            (4097, 1, 64, 3), (1500, 7, 256, 40), (9001, 4, 33, 17), (7000, 2, 16, 40), (6500, 8, 8, 120), (6200, 3, 5, 250), (9001, 5, 7, 131), (6144, 16, 9, 1), (1365, 3, 90, 11), (1366, 3, 90, 11), (4096, 2, 31, 12), (4097, 2, 31, 12), (2731, 3, 200, 9), (128, 4, 900, 3), (129, 4, 900, 3), (257, 1, 6, 5), (9300, 1, 1024, 20), (511, 5, 1024, 6), (585, 7, 2, 19), (2047, 2, 700, 5), (2, 64, 100, 20), (300, 64, 1000, 8)]
 
 
 @pytest.mark.parametrize("t,k,e,h", DISPATCH)
@@ -351,6 +351,29 @@ def test_dispatch_rows_behind_32_bits():
     grad = torch.empty((t * k, 2 * h), dtype=torch.float16, device="cuda")[:, :h]
     bfsp.moe_combine_grad(x, wide, pos, w, grad_rows=grad)
     assert torch.equal(grad[:, 5], (rows[:, 5].float() * 0.25).half()) and torch.equal(grad[-1], (rows[-1].float() * 0.25).half())
+
+
+def test_dispatch_workspace():
+    """A workspace of the caller's, on another stream; one that is too short is
+    refused, and none is needed for few slots."""
+    t, k, e, h = 9000, 2, 77, 24
+    experts, x = _experts(12, t, k, e, drop=0.1), _normal(13, (t, h), torch.bfloat16)
+    want = bfsp.moe_dispatch(experts, e, x)
+    size = bfsp.moe_dispatch_workspace(t, k, e)
+    assert size > 0 and bfsp.moe_dispatch_workspace(4096, k, e) == 0
+    buf = torch.full((size + 64,), 77, dtype=torch.uint8, device="cuda")
+    got = [torch.zeros_like(v) for v in want]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    bfsp.moe_dispatch(experts, e, x, perm=got[0], expert_off=got[1], pos=got[2], rows=got[3], workspace=buf[:size], stream=stream)
+    stream.synchronize()
+    n = int(want[1][-1])
+    assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    assert torch.equal(got[0][:n], want[0][:n]) and torch.equal(got[3][:n], want[3][:n]) and (buf[size:] == 77).all()
+    for bad in (buf[:size - 4], buf[2:2 + size]):
+        with pytest.raises(BfsError) as err:
+            bfsp.moe_dispatch(experts, e, x, workspace=bad)
+        assert err.value.status == bfs.E_INVALID
 
 
 def test_broadcast_inputs():
