@@ -20,7 +20,8 @@
 // have two steps each, and with four rows and more one step, else a wave does
 // (16000 tokens of 4096 bf16, two rows: 120 us with a workgroup and 125 with a
 // wave for each, of 2048 57 and 53; seven rows of 2048: 183 and 191; of 2248,
-// which begin anywhere in a line: 306 and 210).
+// which begin anywhere in a line: 306 and 210), as it does for up to 512 tokens
+// (64, eight rows of 2048: 4.1 and 6.3; 2400: 33 and 38, of 700: 17 and 14).
 // 16384 tokens of eight rows of 2048 bf16, 605 MB: 100 us (6.0 TB/s; a large
 // copy runs at 5.3), its gradient, 1.14 GB, 203 us (5.6).
 #include "op_common.h"
@@ -335,11 +336,11 @@ __device__ __forceinline__ void grad_slots_lines(const CombineParams &P, const T
   }
 }
 
-// W waves take a token.
+// W waves take a token: all of a workgroup, or one.
 template <typename T, int W, bool kStream, bool kLines>
-__global__ void __launch_bounds__(kThreads) combine_grad_kernel(CombineParams P) {
-  __shared__ float part[W > 1 ? W : 1][kMaxK];
-  const int64_t t = ((int64_t)blockIdx.x * kBlockWaves + wave_index()) / W;
+__global__ void __launch_bounds__(W > 1 ? W * kWave : kThreads) combine_grad_kernel(CombineParams P) {
+  __shared__ float part[W][kMaxK];
+  const int64_t t = W > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kBlockWaves + wave_index();
   if (t >= P.n_tokens) return;
   const int lane = lane_index(), wave = wave_index() % W;
   int slot;
@@ -470,10 +471,11 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
         constexpr int W = decltype(waves)::value;
         return launch("moe_combine_grad", !stream_rows ? combine_grad_kernel<T, W, false, false>
                                           : lines ? combine_grad_kernel<T, W, true, true> : combine_grad_kernel<T, W, true, false>,
-                      W > 1 ? n_tokens : (n_tokens + kBlockWaves - 1) / kBlockWaves, kThreads, 0, stream, P);
+                      W > 1 ? n_tokens : (n_tokens + kBlockWaves - 1) / kBlockWaves, W > 1 ? W * kWave : kThreads, 0, stream, P);
       };
       const int64_t whole = width / Chunk<T>::kElems;
-      return whole >= 2 * kThreads || (whole >= kThreads && k >= 4 && !lines) ? run(Int<kBlockWaves>{}) : run(Int<1>{});
+      const bool workgroup = whole >= 2 * kThreads || (whole >= kThreads && k >= 4 && !lines) || (whole >= kWave && n_tokens <= 512);
+      return workgroup ? run(Int<kBlockWaves>{}) : run(Int<1>{});
     });
   });
 }

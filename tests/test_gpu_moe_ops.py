@@ -409,7 +409,7 @@ def _combine_reference(rows, pos, w):
 
 COMBINE = [(1, 1, 1, 1), (1, 8, 64, 4096), (3, 1, 5, 7), (8, 2, 64, 130), (33, 3, 9, 255), (64, 5, 8, 513), (100, 8, 32, 1001),
            (700, 2, 8, 64), (257, 7, 20, 24), (40, 16, 64, 96), (10, 64, 128, 72), (5000, 2, 16, 40), (2, 4, 8, 8200),
-           (7000, 2, 16, 40), (6500, 8, 8, 120), (7001, 5, 9, 17), (6200, 3, 5, 250), (6144, 1, 3, 8), (9001, 7, 5, 129), (6144, 64, 70, 5)]
+           (512, 3, 6, 700), (513, 3, 6, 700), (20, 5, 6, 519), (700, 2, 6, 2600), (7000, 2, 16, 40), (6500, 8, 8, 120), (7001, 5, 9, 17), (6200, 3, 5, 250), (6144, 1, 3, 8), (9001, 7, 5, 129), (6144, 64, 70, 5)]
 
 
 @pytest.mark.parametrize("t,k,e,h", COMBINE)
