@@ -24,7 +24,7 @@
 // stores under way.
 //
 // Bound by memory: 32768 tokens of 4096 bf16 to two experts of 64 each, 806 MB,
-// in 154 us (5.2 TB/s, a large copy's rate), some 9 us of them the ranking.
+// in 150 us (5.4 TB/s, a large copy's rate), some 9 us of them the ranking.
 #include "op_common.h"
 
 using namespace bfsop;

@@ -19,6 +19,7 @@ is wrong.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import struct
 
 import torch
@@ -158,6 +159,7 @@ def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logi
     return grad_logits
 
 
+@functools.lru_cache(maxsize=1024)
 def moe_dispatch_workspace(n_tokens, k, n_experts):
     """Bytes of device memory that a dispatch of these sizes works in."""
     if n_experts > MAX_EXPERTS:
@@ -227,7 +229,7 @@ def moe_dispatch(experts, n_experts, x=None, *, perm=None, expert_off=None, pos=
         _refuse(name, "rows without x")
     if not alone:
         if workspace is None:
-            workspace = experts.new_empty(moe_dispatch_workspace(t, k, n_experts), dtype=torch.uint8)
+            workspace = experts.new_empty((moe_dispatch_workspace(t, k, n_experts) + 3) // 4)
         elif workspace.get_device() != device or not workspace.is_contiguous():
             _refuse(name, "workspace must be a contiguous tensor on the current device")
         ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
@@ -397,10 +399,11 @@ class GradSet:
             self._table = torch.frombuffer(image, dtype=torch.uint8).to(grads[0].device)     # waits for the copy
         self._args = C.addressof(self._set), 0 if self._table is None else self._table.data_ptr()
         self.workspace_bytes = self._set.workspace_bytes
+        self._words = (self.workspace_bytes + 3) // 4
 
     def _buffers(self, name, norm, workspace, stream):
-        device = _device() if self._device is None else self._device
-        if device != _device():
+        device = _device()
+        if device != self._device and self._device is not None:
             _refuse(name, "the gradients are not on the current device")
         handle = _raw_stream(device) if stream is None else _stream(name, stream, device,
                                                                     norm is not None and workspace is not None)
@@ -409,7 +412,7 @@ class GradSet:
         elif norm.dtype is not _F32 or norm.dim() != 0 or norm.get_device() != device:
             _refuse_dense(name, "norm", norm, (), _F32)
         if workspace is None:
-            return norm, norm.new_empty(self.workspace_bytes, dtype=torch.uint8), self.workspace_bytes, handle
+            return norm, norm.new_empty(self._words), self.workspace_bytes, handle
         if workspace.get_device() != device or not workspace.is_contiguous():
             _refuse(name, "workspace must be a contiguous tensor on the current device")
         return norm, workspace, workspace.numel() * workspace.element_size(), handle
@@ -417,7 +420,10 @@ class GradSet:
     def norm(self, norm=None, workspace=None, stream=None):
         """The global norm, a float32 scalar on the device."""
         norm, workspace, size, handle = self._buffers("grad_norm", norm, workspace, stream)
-        _call(bfs._lib.bfs_call, _NORM(5, 6, *self._args, norm.data_ptr(), workspace.data_ptr(), size, handle))
+        address, table = self._args
+        status = bfs._lib.bfs_call(_NORM(5, 6, address, table, norm.data_ptr(), workspace.data_ptr(), size, handle))
+        if status:
+            bfs._check(status)
         return norm
 
     def clip(self, max_norm, norm=None, workspace=None, stream=None):
@@ -425,7 +431,10 @@ class GradSet:
         returns the norm before clipping.  A norm that is not finite (in
         float32) scales by 1."""
         norm, workspace, size, handle = self._buffers("grad_clip", norm, workspace, stream)
-        _call(bfs._lib.bfs_call, _CLIP(6, 7, *self._args, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle))
+        address, table = self._args
+        status = bfs._lib.bfs_call(_CLIP(6, 7, address, table, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle))
+        if status:
+            bfs._check(status)
         return norm
 
 
