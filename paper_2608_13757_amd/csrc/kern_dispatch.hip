@@ -17,8 +17,8 @@
 // group's slots by expert, and the ranking workgroups sum the groups before
 // theirs, or, where that table is long, read sums that one more launch makes.
 // The rows are copied by the ranking workgroups where 512 of them give each
-// wave one part of a row: several then rank the same group, each for itself,
-// and one launch is saved (2048 tokens of 4096 bf16 to 8 experts each: 32 us,
+// wave one part of a row, or a few in the caches: several then rank the same
+// group, each for itself, and one launch is saved (2048 tokens of 4096 bf16 to 8 experts each: 32 us,
 // with the copy in a launch of its own 35; 128 tokens to two: 3.9 us in a single
 // launch).  Beyond, the copy is a launch of its own, whose waves end with their
 // stores under way.
@@ -499,6 +499,13 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       const bool stream_rows = (k + 1) * n_tokens * width * (int64_t)sizeof(T) >= kStreamFrom;
       const int64_t in_group = (n_tokens < P.group / k ? n_tokens : P.group / k) * P.spans;
       P.parts = (int32_t)((in_group + kWaves - 1) / kWaves);
+      const int64_t row_chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
+      const bool narrow = narrow_rows(row_chunks, n_tokens, k);
+      // In the caches a launch less is worth more than a wave for each part of a
+      // row, while five workgroups and more copy a group's rows (8000 tokens of
+      // 2048 bf16 to two: 26.3 us, so 24.6; of 512: 12.7 and 11.9; 32768 of 264 to
+      // four, with four workgroups: 28.4 and 32.2).
+      if (!stream_rows && !narrow && all * 5 <= kBlocks && all * P.parts > kBlocks) P.parts = (int32_t)(kBlocks / all);
       if (all * P.parts <= kBlocks)
         return launch("moe_dispatch", stream_rows ? dispatch_kernel<T, true> : dispatch_kernel<T, false>, all * P.parts, kThreads,
                       lds, stream, P);
@@ -507,8 +514,7 @@ bfs_status bfs_moe_dispatch(const int32_t *experts, int64_t n_tokens, int32_t k,
       s = launch("moe_dispatch", dispatch_kernel<T, false>, all, kThreads, lds, stream, P);
       P.x = x;
       if (s != BFS_OK) return s;
-      const int64_t row_chunks = (width + Chunk<T>::kElems - 1) / Chunk<T>::kElems;
-      if (narrow_rows(row_chunks, n_tokens, k))
+      if (narrow)
         return with_group(row_chunks, [&](auto g) {
           constexpr int G = decltype(g)::value;
           return launch("moe_dispatch", copy_narrow_kernel<T, G>, (n_tokens + kCopyThreads / G - 1) / (kCopyThreads / G),

@@ -290,7 +290,7 @@ def _dispatch_reference(experts, e):
 # around one wave's batch, one group (1024 slots) and one launch's limit (8192)
 DISPATCH = [(0, 2, 5, 8), (1, 1, 1, 1), (1, 8, 64, 4096), (3, 1, 5, 7), (8, 2, 64, 130), (63, 1, 3, 16), (65, 1, 1, 33),
             (128, 8, 64, 24), (1024, 1, 17, 8), (1025, 1, 17, 9), (512, 2, 1024, 12), (342, 3, 300, 65), (4096, 1, 64, 4),
-            (4097, 1, 64, 3), (1500, 7, 256, 40), (9001, 4, 33, 17), (7000, 2, 16, 40), (6500, 8, 8, 120), (6200, 3, 5, 250), (9001, 5, 7, 131), (6144, 16, 9, 1), (1365, 3, 90, 11), (1366, 3, 90, 11), (4096, 2, 31, 12), (4097, 2, 31, 12), (2731, 3, 200, 9), (128, 4, 900, 3), (129, 4, 900, 3), (257, 1, 6, 5), (9300, 1, 1024, 20), (511, 5, 1024, 6), (585, 7, 2, 19), (2047, 2, 700, 5), (2, 64, 100, 20), (300, 64, 1000, 8)]
+            (4097, 1, 64, 3), (1500, 7, 256, 40), (9001, 4, 33, 17), (7000, 2, 16, 40), (6500, 8, 8, 120), (6200, 3, 5, 250), (9001, 5, 7, 131), (6144, 16, 9, 1), (6000, 2, 31, 300), (4100, 3, 17, 1030), (30000, 3, 12, 260), (1365, 3, 90, 11), (1366, 3, 90, 11), (4096, 2, 31, 12), (4097, 2, 31, 12), (2731, 3, 200, 9), (128, 4, 900, 3), (129, 4, 900, 3), (257, 1, 6, 5), (9300, 1, 1024, 20), (511, 5, 1024, 6), (585, 7, 2, 19), (2047, 2, 700, 5), (2, 64, 100, 20), (300, 64, 1000, 8)]
 
 
 @pytest.mark.parametrize("t,k,e,h", DISPATCH)
