@@ -18,10 +18,10 @@
 // theirs, or, where that table is long, read sums that one more launch makes.
 // The rows are copied by the ranking workgroups where 512 of them give each
 // wave one part of a row, or a few in the caches: several then rank the same
-// group, each for itself, and one launch is saved (2048 tokens of 4096 bf16 to 8 experts each: 32 us,
-// with the copy in a launch of its own 35; 128 tokens to two: 3.9 us in a single
-// launch).  Beyond, the copy is a launch of its own, whose waves end with their
-// stores under way.
+// group, each for itself, and one launch is saved (2048 tokens of 4096 bf16 to
+// eight experts each: 32 us, with the copy in a launch of its own 35; 128 tokens
+// to two: 3.9 us in a single launch).  Beyond, the copy is a launch of its own,
+// whose waves end with their stores under way.
 //
 // Bound by memory: 32768 tokens of 4096 bf16 to two experts of 64 each, 806 MB,
 // in 150 us (5.4 TB/s, a large copy's rate), some 9 us of them the ranking.
