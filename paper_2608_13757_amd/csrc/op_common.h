@@ -133,41 +133,43 @@ __device__ __forceinline__ uint32_t ror16(uint32_t x) {
 }
 
 // Reductions over groups of G consecutive lanes (16 or 64); every lane gets
-// the same result: each step pairs values symmetrically.
+// the same result: inside a row of 16 each step pairs values symmetrically, and
+// four rows are joined in the last one's last lane.  none: f(x, none) is x.
 template <int G, typename F>
-__device__ __forceinline__ uint32_t group_reduce(uint32_t x, F f) {
+__device__ __forceinline__ uint32_t group_reduce(uint32_t x, uint32_t none, F f) {
   static_assert(G == 16 || G == 64, "groups of 16 or 64 lanes");
   x = f(x, ror16<8>(x));
   x = f(x, ror16<4>(x));
   x = f(x, ror16<2>(x));
   x = f(x, ror16<1>(x));
-  if (G == 64) {                                   // the four rows' results, in scalar registers
-    auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); };
-    x = f(f(row(0), row(16)), f(row(32), row(48)));
+  if (G == 64) {
+    x = f(x, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, 0x142, 0xa, 0xf, false));      // row_bcast:15
+    x = f(x, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, 0x143, 0xc, 0xf, false));      // row_bcast:31
+    x = (uint32_t)__builtin_amdgcn_readlane((int)x, kWave - 1);
   }
   return x;
 }
 
 template <int G>
 __device__ __forceinline__ uint32_t group_max(uint32_t x) {
-  return group_reduce<G>(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  return group_reduce<G>(x, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
 }
 
 template <int G>
 __device__ __forceinline__ uint32_t group_min(uint32_t x) {
-  return group_reduce<G>(x, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+  return group_reduce<G>(x, 0xffffffffu, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
 }
 
 template <int G>
 __device__ __forceinline__ float group_maxf(float x) {
-  return __uint_as_float(group_reduce<G>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+  return __uint_as_float(group_reduce<G>(__float_as_uint(x), 0xff800000u, [](uint32_t a, uint32_t b) {      // -inf
     return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
   }));
 }
 
 template <int G>
 __device__ __forceinline__ float group_sum(float x) {
-  return __uint_as_float(group_reduce<G>(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+  return __uint_as_float(group_reduce<G>(__float_as_uint(x), 0x80000000u, [](uint32_t a, uint32_t b) {      // -0
     return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
   }));
 }
