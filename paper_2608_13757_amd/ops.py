@@ -349,8 +349,11 @@ class GradSet:
     a table of the tensors on the device, and their memory: a gradient that is
     allocated anew needs a new set.  A gradient named twice counts twice in the
     norm; a set whose outputs overlap (that one in place, say) is not clipped.
-    Making one copies the table (it waits for
-    the copy and cannot be captured); the calls can be."""
+    Making one copies the table (it waits for the copy and cannot be captured);
+    the calls can be.  A set may be dropped while a call of it is under way, on
+    whatever stream: its memory is used again only behind that stream's work.
+    A stream given by its handle has to exist until the set is gone, and a set
+    whose calls were captured has to be kept as long as the graph."""
 
     def __init__(self, grads, out=None):
         name = "GradSet"
@@ -384,6 +387,9 @@ class GradSet:
         # aliases: the memory stays even where a tensor's data is exchanged
         self._keep = [t.detach() for t in [*grads, *outs]]
         self._device = devices.pop() if devices else None
+        # The stream that the table's memory belongs to, and the other ones that calls ran on.
+        self._made_on = None if self._device is None else _raw_stream(self._device)
+        self._used_on = set()
         n = len(grads)
         arrays = (struct.pack("%dP" % n, *[g.data_ptr() for g in grads]), struct.pack("%dP" % n, *[o.data_ptr() for o in outs]),
                   struct.pack("%dq" % n, *sizes), struct.pack("%di" % n, *types),
@@ -397,9 +403,21 @@ class GradSet:
             image = bytearray(size)
             _call(table, *arrays, C.byref(self._set), (C.c_char * size).from_buffer(image), size)
             self._table = torch.frombuffer(image, dtype=torch.uint8).to(grads[0].device)     # waits for the copy
+            self._keep.append(self._table)
         self._args = C.addressof(self._set), 0 if self._table is None else self._table.data_ptr()
         self.workspace_bytes = self._set.workspace_bytes
         self._words = (self.workspace_bytes + 3) // 4
+
+    def _record(self, stream, handle):
+        """The allocator is told that a stream uses the set's memory: once for
+        each stream, it holds until the memory goes back."""
+        if stream is None:
+            stream = torch.cuda.current_stream()
+        elif isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream)
+        for t in self._keep:
+            t.record_stream(stream)
+        self._used_on.add(handle)
 
     def _buffers(self, name, norm, workspace, stream):
         device = _device()
@@ -411,10 +429,12 @@ class GradSet:
             norm = torch.empty((), dtype=_F32, device="cuda")
         elif norm.dtype is not _F32 or norm.dim() != 0 or norm.get_device() != device:
             _refuse_dense(name, "norm", norm, (), _F32)
+        if workspace is not None and (workspace.get_device() != device or not workspace.is_contiguous()):
+            _refuse(name, "workspace must be a contiguous tensor on the current device")
+        if handle != self._made_on and handle not in self._used_on:
+            self._record(stream, handle)
         if workspace is None:
             return norm, norm.new_empty(self._words), self.workspace_bytes, handle
-        if workspace.get_device() != device or not workspace.is_contiguous():
-            _refuse(name, "workspace must be a contiguous tensor on the current device")
         return norm, workspace, workspace.numel() * workspace.element_size(), handle
 
     def norm(self, norm=None, workspace=None, stream=None):

@@ -210,3 +210,36 @@ def test_refusals():
         with pytest.raises(BfsError) as e:
             call()
         assert e.value.status == bfs.E_INVALID
+
+
+@pytest.mark.parametrize("call", ["one_shot", "handle", "current"])
+def test_set_dropped_while_another_stream_uses_it(call):
+    """The set's table is not given to the allocations that follow its release
+    while a stream other than the set's is still to run the call."""
+    grads = _grads(12, [70_001, 33, 5000], [torch.bfloat16])
+    want = [g.double() * min(1.0, 0.5 / (_norm64(grads) + 1e-6)) for g in grads]
+    out, norm = torch.zeros(75_034, device="cuda"), torch.zeros((), device="cuda")
+    s = GradSet(grads, out=out)
+    s.clip(0.5)                                        # (the kernels are loaded)
+    workspace = torch.empty(s.workspace_bytes, dtype=torch.uint8, device="cuda")
+    out.zero_()
+    del s
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)                  # milliseconds, before the call's kernels
+    if call == "one_shot":
+        bfsp.grad_clip(grads, 0.5, out=out, norm=norm, workspace=workspace, stream=stream)
+    elif call == "handle":
+        GradSet(grads, out=out).clip(0.5, norm=norm, workspace=workspace, stream=stream.cuda_stream)
+    else:
+        s = GradSet(grads, out=out)
+        with torch.cuda.stream(stream):
+            s.clip(0.5, norm=norm, workspace=workspace)
+        del s
+    zeros = [torch.zeros(n, dtype=torch.uint8, device="cuda") for n in [512, 1024, 2048, 4096, 8192] * 40]
+    stream.synchronize()
+    _check_norm(norm, grads)
+    for o, g, w in zip(out.split([g.numel() for g in grads]), grads, want):
+        assert bool(((o.double() - w).abs() <= w.abs() * 4 * U).all())
+    assert all((z == 0).all() for z in zeros[:5])

@@ -231,3 +231,61 @@ def test_package_imports_without_the_operators():
     code = ("import sys; import paper_2608_13757_amd as p; assert 'torch' not in sys.modules; p.lib(); "
             "assert 'torch' not in sys.modules\ntry:\n p.no_such_name\nexcept AttributeError: pass\nelse: raise SystemExit(1)")
     subprocess.run([sys.executable, "-c", code], check=True)
+
+
+def _on_device(torch, *args, **kw):
+    """A tensor of the host that says it is on device 0."""
+    class T(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return 0
+    return torch.zeros(*args, **kw).as_subclass(T)
+
+
+@pytest.mark.parametrize("given", ["handle", "current"])
+def test_set_of_gradients_belongs_to_the_streams_that_use_it(given, monkeypatch):
+    """Calls on another stream than the set was made on: before the first of
+    each stream is enqueued the allocator knows that it uses the table and the
+    gradients, so that a set dropped at once (the one-shot calls do) is not
+    given away under the kernels.  On the host, with the launch left out."""
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+
+    from paper_2608_13757_amd import ops
+    real, current, events = bfs.lib(), [0], []
+    monkeypatch.setattr(ops, "_device", lambda: 0)
+    monkeypatch.setattr(ops, "_raw_stream", lambda device: current[0])
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: events.append((t.data_ptr(), s)), raising=False)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: handle)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: current[0])
+    monkeypatch.setattr(bfs, "_lib", SimpleNamespace(bfs_grad_table=real.bfs_grad_table,
+                                                     bfs_call=lambda words: events.append("call") or 0))
+    grads = [_on_device(torch, 50), _on_device(torch, 7, dtype=torch.bfloat16)]
+    flat = _on_device(torch, 57)
+    kw = dict(norm=_on_device(torch, ()), workspace=_on_device(torch, 1024, dtype=torch.float64))
+
+    def run(method, *args, on, **more):
+        events.clear()
+        if given == "current":
+            current[0] = on
+        else:
+            kw["stream"] = on
+        method(*args, **kw, **more)
+
+    s = ops.GradSet(grads, out=flat)
+    memory = {s._args[1], flat.data_ptr(), flat[50:].data_ptr(), *(g.data_ptr() for g in grads)}
+    run(s.norm, on=0)
+    assert events == ["call"]                          # the set's own stream
+    for method, args in ((s.norm, ()), (s.clip, (1.0,))):
+        run(method, *args, on=7)
+        if method == s.norm:
+            assert events[-1] == "call" and set(events[:-1]) == {(p, 7) for p in memory}
+        else:
+            assert events == ["call"]                  # known already
+    run(s.clip, 1.0, on=9)
+    assert events[-1] == "call" and {e[1] for e in events[:-1]} == {9}
+    current[0] = 0
+    if given == "handle":                              # a set that nothing but the call holds
+        run(ops.grad_clip, grads, 1.0, on=7, out=flat)
+        assert events[-1] == "call" and len({e[0] for e in events[:-1]}) == 5 and {e[1] for e in events[:-1]} == {7}
