@@ -136,7 +136,7 @@ def moe_route_grad(logits, experts, grad_weights, *, renormalize=True, grad_logi
     dtype = DTYPES.get(logits.dtype)
     if dtype is None:
         _refuse_type(name, "logits", logits)
-    k = experts.shape[-1]
+    k = experts.shape[-1] if experts.shape else 1
     shape = (t, k)
     if experts.dtype is not _I32 or experts.shape != shape or experts.get_device() != device or not experts.is_contiguous():
         _refuse_dense(name, "experts", experts, shape, _I32)
@@ -311,7 +311,7 @@ def moe_combine_grad(grad_y, rows, pos, weights, *, grad_rows=None, grad_weights
     rows_stride, unit = rows.stride()
     if unit != 1 and width > 1:
         _refuse_matrix(name, "rows", rows)
-    k = pos.shape[-1]
+    k = pos.shape[-1] if pos.shape else 1
     slots = (t, k)
     if pos.dtype is not _I32 or pos.shape != slots or pos.get_device() != device or not pos.is_contiguous():
         _refuse_dense(name, "pos", pos, slots, _I32)

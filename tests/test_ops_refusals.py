@@ -289,3 +289,19 @@ def test_set_of_gradients_belongs_to_the_streams_that_use_it(given, monkeypatch)
     if given == "handle":                              # a set that nothing but the call holds
         run(ops.grad_clip, grads, 1.0, on=7, out=flat)
         assert events[-1] == "call" and len({e[0] for e in events[:-1]}) == 5 and {e[1] for e in events[:-1]} == {7}
+
+
+@pytest.mark.parametrize("shape", [(), (4,), (1, 4, 2), (3, 2), (0,)])
+def test_ids_that_are_no_matrix(shape, monkeypatch):
+    """Ids and positions of any other shape are refused as BfsError, a number
+    of no dimension too.  On the host, before anything would be launched."""
+    torch = pytest.importorskip("torch")
+    from paper_2608_13757_amd import ops
+    monkeypatch.setattr(ops, "_device", lambda: 0)
+    monkeypatch.setattr(ops, "_raw_stream", lambda device: 0)
+    ids, w, x = _on_device(torch, shape, dtype=torch.int32), _on_device(torch, 4, 2), _on_device(torch, 4, 16)
+    for call in (lambda: ops.moe_route_grad(x, ids, w), lambda: ops.moe_combine_grad(x, x, ids, w),
+                 lambda: ops.moe_combine(x, ids, w), lambda: ops.moe_dispatch(ids, 8, x)):
+        with pytest.raises(BfsError) as e:
+            call()
+        assert e.value.status == bfs.E_INVALID
