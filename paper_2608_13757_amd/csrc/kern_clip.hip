@@ -19,7 +19,7 @@
 // tensors took six launches and 510 us).
 //
 // 2^28 bf16 gradients in 290 tensors into fp32: 371 us, 5.8 TB/s over both
-// passes (a large copy's rate is 5.3); 2^20 fp32 in 24: 7.9 us, two short
+// passes (a large copy's rate is 5.3); 2^20 fp32 in 24: 7.4 us, two short
 // launches.
 #include <algorithm>
 #include <cmath>
@@ -33,7 +33,6 @@ using namespace bfsop;
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 8;                        // accesses of a lane in flight
 // Elements a workgroup takes at once, less where the tensors would leave
 // workgroups idle (2^28 bf16 in 290 tensors: 389 us with 8192, 415 with 16384,
 // whose last chunks are less even over the workgroups).
@@ -48,6 +47,12 @@ constexpr int kBlocks = 1024, kMostBlocks = 4096, kChunksEach = 4;
 // these; 2^26 bf16: 27 and 30).  A clipping's first pass leaves there what it
 // can for the second.
 constexpr int64_t kStreamNorm = 256 << 20;
+// LDS that a workgroup of either pass takes, though it needs little of it, so
+// that four are resident on a compute unit (160 KB): with seven and eight, as the
+// registers allow, memory serves more places at once and is slower (2^28 bf16 into
+// fp32: 380 us, so 371, the norm alone 89.6 and 86.1; 2^27 fp16 184 and 181; 2^20
+// fp32 7.5 and 7.4).
+constexpr size_t kHeldLds = 39 << 10;
 constexpr int64_t kMaxElements = (int64_t)1 << 43;
 constexpr double kEps = 1e-6;
 
@@ -97,11 +102,12 @@ __device__ __forceinline__ double block_sum(double s) {
   return t;
 }
 
-// f on this lane's vectors while U accesses are whole, then with U / 2 of them.
+// f on this lane's vectors, of which at most 2 U - 1 are left: U of them with
+// all accesses issued before the first is used, then U / 2, ...
 template <int U, bool kStream, typename Vec, int V, typename T, typename F>
 __device__ __forceinline__ void each_vector(const T *g, int64_t at, int64_t end, F f) {
   constexpr int kStep = kThreads * V;
-  while (at + (U - 1) * kStep < end) {
+  if (at + (U - 1) * kStep < end) {
     Vec v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -111,24 +117,25 @@ __device__ __forceinline__ void each_vector(const T *g, int64_t at, int64_t end,
 #pragma unroll
     for (int u = 0; u < U; ++u) f(at + u * kStep, v[u]);
     at += U * kStep;
-    if (U < kUnroll) break;                       // fewer than U accesses are left
   }
   if constexpr (U > 1) each_vector<U / 2, kStream, Vec, V>(g, at, end, f);
 }
 
 // Chunk c of a tensor of n elements at g, `chunks` of them in all, whose first
-// whole line (of `aligned`: g itself or the output) begins at element head:
+// whole line (of g itself or of the output) begins at element head:
 // chunks begin with a line, the first one at element 0, the last one takes
-// what is left.  f(first element, vector) for this lane's vectors, up to
-// kUnroll accesses issued before the first is used, one(element) for the
-// elements that no vector holds.
+// what is left.  f(first element, vector) for this lane's vectors, those of a
+// whole chunk in flight at once (eight accesses where a vector has four elements,
+// four where it has eight), one(element) for the elements that no vector holds.
 template <bool kStream, typename Vec, int V, typename T, typename F, typename One>
 __device__ __forceinline__ void each_element(const T *g, int64_t n, int head, int64_t chunk, int c, int chunks, F f, One one) {
   const int64_t from = head + c * chunk, to = c + 1 == chunks || from + chunk > n ? n : from + chunk;
   if (c == 0 && (int)threadIdx.x < head) one((int64_t)threadIdx.x);
   if (from >= to) return;
   const int64_t end = to - (to - from) % V;
-  each_vector<kUnroll, kStream, Vec, V>(g, from + (int64_t)threadIdx.x * V, end, f);
+  constexpr int kMost = (int)(kMaxChunk / (kThreads * V));        // vectors of a lane in a chunk, at most
+  static_assert(kMost * kThreads * V == kMaxChunk && (kMost & (kMost - 1)) == 0, "a chunk's vectors, by halves");
+  each_vector<kMost, kStream, Vec, V>(g, from + (int64_t)threadIdx.x * V, end, f);
   if (end + threadIdx.x < to) one(end + threadIdx.x);
 }
 
@@ -360,7 +367,7 @@ bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *
     double *partial = static_cast<double *>(workspace);
     if (set->n_blocks > 0)
       st = launch("grad_norm", set->grad_bytes >= kStreamNorm ? square_kernel<true> : square_kernel<false>, set->n_blocks, kThreads,
-                  0, stream, table_of(*set, dev_image), partial);
+                  kHeldLds, stream, table_of(*set, dev_image), partial);
     if (st != BFS_OK) return st;
     return launch("grad_norm", norm_kernel, 1, kThreads, 0, stream, partial, set->n_blocks, norm);
   });
@@ -377,9 +384,9 @@ bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double 
     double *partial = static_cast<double *>(workspace);
     if (set->n_blocks == 0) return norm ? launch("grad_clip", norm_kernel, 1, kThreads, 0, stream, partial, 0, norm) : BFS_OK;
     const Table t = table_of(*set, dev_image);
-    st = launch("grad_clip", square_kernel<false>, set->n_blocks, kThreads, 0, stream, t, partial);
+    st = launch("grad_clip", square_kernel<false>, set->n_blocks, kThreads, kHeldLds, stream, t, partial);
     if (st != BFS_OK) return st;
-    return launch("grad_clip", clip_kernel, set->n_blocks, kThreads, 0, stream,
+    return launch("grad_clip", clip_kernel, set->n_blocks, kThreads, kHeldLds, stream,
                   t, partial, max_norm, norm);
   });
 }
