@@ -622,3 +622,46 @@ def test_refusals():
                  lambda: bfsp.moe_combine(rows, ids, w, stream=other)):
         with pytest.raises(BfsError):
             call()
+
+
+def _check_dispatch(t, k, e, h, dtype, shift, drop, skew=False):
+    """A dispatch into the middle of a buffer against the definition; what lies
+    outside the rows that have a slot stays."""
+    experts = _experts(t + e, t, k, e, drop=drop, skew=skew)
+    x = _normal(h, (1 << 10, h), dtype)[torch.arange(t, device="cuda") * 7919 % (1 << 10)]
+    x[:, 0] = torch.arange(t, device="cuda") % 211
+    x[:, -1] = torch.arange(t, device="cuda") // 211 % 211
+    buf = torch.full((t * k * h + 64 + shift,), 77, dtype=dtype, device="cuda")
+    perm = torch.full((t * k,), -9, dtype=torch.int32, device="cuda")
+    perm, off, pos, rows = bfsp.moe_dispatch(experts, e, x, perm=perm, rows=buf[shift:shift + t * k * h].view(t * k, h))
+    ref_perm, ref_off, ref_pos = _dispatch_reference(experts, e)
+    n = len(ref_perm)
+    assert np.array_equal(off.cpu().numpy(), ref_off) and np.array_equal(pos.cpu().numpy(), ref_pos)
+    assert np.array_equal(perm[:n].cpu().numpy(), ref_perm) and (perm[n:] == -9).all()
+    assert torch.equal(rows[:n], x[torch.from_numpy(ref_perm).cuda().long()])
+    assert (buf[:shift] == 77).all() and (buf[shift + n * h:] == 77).all()
+
+
+@pytest.mark.parametrize("t,k,e,h,dtype,shift,drop", [
+    (2048, 8, 64, 4096, torch.bfloat16, 0, 0.0), (2048, 8, 64, 4096, torch.bfloat16, 3, 0.15), (2048, 8, 64, 4095, torch.float16, 1, 0.15),
+    (2048, 4, 31, 4096, torch.float32, 0, 0.1), (1200, 6, 300, 8190, torch.bfloat16, 5, 0.3), (1600, 7, 1000, 4097, torch.float16, 0, 0.0)])
+def test_dispatch_past_the_caches_by_the_ranking_workgroups(t, k, e, h, dtype, shift, drop):
+    """96 MiB and more, of so few long rows that the workgroups that rank a
+    group's slots copy them too (a wave for each part of a row, 512 workgroups
+    at most), with a table of counts and, up to 8192 slots, without one."""
+    steps = -(-h * dtype.itemsize // 1024)
+    spans, group = max(2, min(steps, -(-512 // t))), 1024 // k
+    assert (k + 1) * t * h * dtype.itemsize >= 96 << 20 and steps >= 4
+    assert -(-t // group) * -(-min(t, group) * spans // 8) <= 512
+    _check_dispatch(t, k, e, h, dtype, shift, drop)
+
+
+@pytest.mark.parametrize("t,k,e,h,drop", [(4700, 2, 300, 8, 0.1), (6400, 2, 300, 24, 0.0), (1900, 7, 290, 9, 0.2), (9217, 1, 400, 5, 0.1),
+                                          (6000, 3, 200, 8, 0.1), (8700, 1, 455, 3, 0.0), (26_600, 1, 150, 4, 0.3), (22_000, 2, 90, 3, 0.1)])
+def test_dispatch_sums_of_many_groups(t, k, e, h, drop):
+    """More than 8192 slots whose counts every ranking workgroup sums by
+    itself: of more groups than its threads load ahead."""
+    groups = -(-t // (1024 // k))
+    assert t * k > 8192 and 1024 <= groups * e <= 4096 and groups > 8 * (512 // e)
+    for skew in (False, True):
+        _check_dispatch(t, k, e, h, torch.bfloat16, 1, drop, skew)
