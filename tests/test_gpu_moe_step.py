@@ -12,6 +12,7 @@ torch = pytest.importorskip("torch")
 import paper_2608_13757_amd as bfsp  # noqa: E402
 from oracle.mathref import adamw_step  # noqa: E402
 from paper_2608_13757_amd import GradSet, Plan, bfs  # noqa: E402
+from paper_2608_13757_amd.ops import DISPATCH_ALONE  # noqa: E402
 from tests.gpu_util import trip_tensors  # noqa: E402
 from workloads import ADAM_HP, adamw_default_wg, adamw_program, adamw_worklist, moe_program, moe_worklist  # noqa: E402
 
@@ -252,3 +253,99 @@ def test_two_threads_at_once():
     assert not errors
     for a, b in zip(got, want):
         assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+# Dispatches that work in a table of counts; of the second a launch of its own sums it.
+WITH_TABLE = [dict(t=6000, e=64, k=2, h=128, dtype=torch.bfloat16), dict(t=9000, e=300, k=3, h=72, dtype=torch.float16)]
+
+
+def _with_table(t, e, k, **_):
+    assert t * k > DISPATCH_ALONE and bfsp.moe_dispatch_workspace(t, k, e) > 0
+    return -(-t // (1024 // k)) * e                    # counts of the table
+
+
+def test_tables_of_counts_on_two_streams():
+    """The calls' own workspaces, and one for each stream given by argument."""
+    assert _with_table(**WITH_TABLE[0]) <= 4096 < _with_table(**WITH_TABLE[1])
+    for sizes in (WITH_TABLE, WITH_TABLE[::-1], WITH_TABLE[1:] * 2):
+        steps = [_Step(**z, seed=11 * i) for i, z in enumerate(sizes)]
+        for i, s in enumerate(steps):
+            s.refill(i + 1)
+        want = [s.run() for s in steps]
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        tables = [torch.full((bfsp.moe_dispatch_workspace(z["t"], z["k"], z["e"]),), 0xff, dtype=torch.uint8, device="cuda") for z in sizes]
+        outs = [[torch.zeros_like(v) for v in w[2:6]] for w in want]
+        torch.cuda.synchronize()
+        got = [None, None]
+        for _ in range(4):
+            for i, (s, st) in enumerate(zip(steps, streams)):
+                with torch.cuda.stream(st):
+                    got[i] = s.run()
+                perm, off, pos, rows = outs[i]
+                bfsp.moe_dispatch(want[i][0], s.e, s.x, perm=perm, expert_off=off, pos=pos, rows=rows, workspace=tables[i], stream=st)
+        torch.cuda.synchronize()
+        for a, b, c in zip(got, want, outs):
+            assert all(torch.equal(p, q) for p, q in zip(a, b))
+            n = int(b[3][-1])
+            assert 0 < n == b[4].numel() - int((b[4] < 0).sum())
+            assert torch.equal(c[1], b[3]) and torch.equal(c[2], b[4]) and torch.equal(c[0][:n], b[2][:n]) and torch.equal(c[3][:n], b[5][:n])
+
+
+def test_tables_of_counts_in_two_threads():
+    """Two host threads, each with its own stream and buffers."""
+    steps = [_Step(**z, seed=9 * i) for i, z in enumerate(WITH_TABLE)]
+    for i, (s, z) in enumerate(zip(steps, WITH_TABLE)):
+        _with_table(**z)
+        s.refill(i + 3)
+    want = [s.run() for s in steps]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    got[i] = steps[i].run()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:          # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for a, b in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+@pytest.mark.parametrize("sizes", WITH_TABLE, ids=lambda z: f"{z['t']}x{z['k']}")
+def test_tables_of_counts_captured(sizes):
+    """Two graphs whose dispatches have a table each, replayed in turn and on
+    two streams at once, with new inputs each time."""
+    _with_table(**sizes)
+    steps = [_Step(**sizes), _Step(**sizes, seed=50)]
+    graphs, outs = [], []
+    for s in steps:
+        s.refill(1)
+        s.run()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(s.run())
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for n in range(4):
+        for i, s in enumerate(steps):
+            s.refill(10 * n + i + 2)
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, streams):
+            if n % 2:
+                with torch.cuda.stream(st):
+                    g.replay()
+            else:
+                g.replay()
+        torch.cuda.synchronize()
+        for s, got in zip(steps, outs):
+            for q, (a, b) in enumerate(zip(got, s.run())):
+                assert torch.equal(a, b), (n, q)
