@@ -190,29 +190,33 @@ __device__ __forceinline__ void rank_slots(const DispatchParams &P, const int (&
   }
 }
 
-// Slots by expert of the groups before g, and of all groups.  With fewer
-// experts than threads several threads (`share`) share an expert's groups.  Of
+// Slots by expert of the groups before g, and of all groups.  Several threads
+// (`share`) share an expert's groups where that leaves no thread without one.  Of
 // a table of some length the first counts of a thread are on their way while it
-// counts its own slots (8000 tokens to eight experts of 64: 23.4 -> 21.3 us; 2000
-// to four of 8, a table of 64 counts: 9.1 and 9.6).
+// counts its own slots (rows of 64 bf16, 8000 tokens to eight experts of 64, 4032
+// counts: 11.8 -> 10.5 us; 2400 to four of 16, 160 counts: 8.0 and 8.3).
 struct GroupSums {
   static constexpr int kAhead = 8, kAheadFrom = 1024;
-  int share, my, e0;
+  int share, my, e;              // this thread: expert e, groups my, my + share, ...
   bool table, early;
   uint32_t ahead[kAhead];
 
   __device__ __forceinline__ void load(const DispatchParams &P) {
+    // There are kAlone / kGroupSlots + 1 groups at least, so that a table which is
+    // summed here has no more experts than a workgroup threads.
+    static_assert(kSumEntries / (kAlone / kGroupSlots + 1) <= kThreads, "a thread for each expert");
     const int E = P.n_experts, t = (int)threadIdx.x;
     table = P.n_groups * (int64_t)E > kSumEntries;
     early = !table && P.n_groups * E >= kAheadFrom;
-    share = E < kThreads ? kThreads / E : 1;
+    if (table) return;
+    share = kThreads / E;
     my = t / E;
-    e0 = share > 1 ? t - my * E : t;
+    e = t - my * E;
     if (!early) return;
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int i = (share > 1 ? my : 0) + u * share;
-      ahead[u] = e0 < E && my < share && i < P.n_groups ? P.counts[i * E + e0] : 0;
+      const int i = my + u * share;
+      ahead[u] = my < share && i < P.n_groups ? P.counts[i * E + e] : 0;
     }
   }
 
@@ -224,12 +228,12 @@ struct GroupSums {
         total[e] = P.counts[(int64_t)P.n_groups * E + e];
       }
     } else {
-      for (int e = (int)threadIdx.x; e < E; e += kThreads) before[e] = total[e] = 0;
+      if (my == 0) before[e] = total[e] = 0;
       __syncthreads();
-      for (int e = e0; e < E && my < share; e += share > 1 ? E : kThreads) {
+      if (my < share) {
         uint32_t all = 0, mine = 0;
-        int i = share > 1 ? my : 0;
-        if (early && e == e0) {
+        int i = my;
+        if (early) {
 #pragma unroll
           for (int u = 0; u < kAhead; ++u, i += share) {
             all += ahead[u];
