@@ -463,11 +463,12 @@ bfs_status bfs_moe_combine_grad(const void *grad_y, int32_t dtype, int64_t n_tok
  * may then be the gradient itself, or is fp32 (a part of the AdamW family's
  * flat gradient, say).  Gradients may share memory; an output shares none with
  * another output or another gradient, or bfs_grad_clip refuses the set
- * (bfs_grad_norm does not read the outputs).  bfs_grad_table fills *set and, where image is given,
- * writes the table of set->image_bytes bytes to it (host memory; call once
- * with NULL for the size).  The caller lays the table into device memory
- * (aligned to 16 bytes), which, like the tensors, must stay as it is while
- * calls use it.  The calls read *set and change nothing in it.  At most 2^43
+ * (bfs_grad_norm does not read the outputs).  bfs_grad_table fills *set and,
+ * where image is given, writes the table of set->image_bytes bytes to it (host
+ * memory; call once with NULL for the size).  The caller lays the table into
+ * device memory (aligned to 16 bytes), which, like the tensors, must stay as it
+ * is until the calls that use it have completed, and as long as a graph that
+ * captured one.  The calls read *set and change nothing in it.  At most 2^43
  * elements in all.
  */
 typedef struct {
@@ -493,8 +494,9 @@ bfs_status bfs_grad_norm(const bfs_grad_set *set, const void *dev_image, float *
 
 /*
  * outs[i] = grads[i] * min(1, max_norm / (norm + 1e-6)).  Where the norm is
- * not finite (in fp32) the scale is 1.  norm: NULL, or where the norm (before clipping)
- * goes.  max_norm >= 0.
+ * not finite in fp32, as it is reported, the scale is 1, also where only fp32
+ * does not hold it: gradients beside an infinite norm are as they were.  norm:
+ * NULL, or where the norm (before clipping) goes.  max_norm >= 0.
  */
 bfs_status bfs_grad_clip(const bfs_grad_set *set, const void *dev_image, double max_norm, float *norm, void *workspace,
                          int64_t workspace_bytes, struct ihipStream_t *stream);

@@ -7,8 +7,10 @@
 // fp32's range from 2^64 on, and the sum is as long as the model), each
 // workgroup over its own chunks in their order, the workgroups' sums in the
 // order of the workgroups: the same bits in every run.  A norm that is not
-// finite (in fp32, as it is reported) leaves in-place gradients as they are and copies them (cast) to a
-// separate output, so that the caller sees them next to the norm that says so.
+// finite in fp32, as it is reported, leaves in-place gradients as they are and
+// copies them (cast) to a separate output, so that the caller sees them next to
+// the norm that says so: an infinite norm always has unscaled gradients beside it,
+// whether the 64-bit sum held it or not.
 //
 // Two passes over the gradients, since the scale depends on all of them;
 // bound by memory.  The second goes over the chunks in the opposite order, so
@@ -18,9 +20,10 @@
 // number (as launch arguments, 128 tensors a launch, 2^28 bf16 gradients in 290
 // tensors took six launches and 510 us).
 //
-// 2^28 bf16 gradients in 290 tensors into fp32: 371 us, 5.8 TB/s over both
-// passes (a large copy's rate is 5.3); 2^20 fp32 in 24: 7.4 us, two short
-// launches.
+// 2^28 bf16 gradients in 290 tensors into fp32: 370 us, 5.8 TB/s over both
+// passes (a large copy's rate is 5.3; 408 us on another device, on which the
+// comparisons of chunks, workgroups, orders and stores below were made); 2^20 fp32
+// in 24: 7.4 us, two short launches.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -34,17 +37,19 @@ namespace {
 
 constexpr int kThreads = 256;
 // Elements a workgroup takes at once, less where the tensors would leave
-// workgroups idle (2^28 bf16 in 290 tensors: 389 us with 8192, 415 with 16384,
+// workgroups idle (2^28 bf16 in 290 tensors: 408 us with 8192, 422 with 16384,
 // whose last chunks are less even over the workgroups).
 constexpr int64_t kMaxChunk = 8192, kMinChunk = 2048;
 // Workgroups: 1024, from four chunks for each of 4096 on these (clipping bf16,
-// 2^28: 410 us with 1024, 390 with 4096; 2^27: 198 and 189; 2^26: 91 and 97).
+// 2^28: 413 us with 1024, 408 with 4096; fp32 596 and 586; 2^26 bf16, which would
+// have two for each: 91 and 97).
 // Numbers between leave a part of the device idle at the end (2^25 with 1030
 // of them 51 us, with 1024 48).
 constexpr int kBlocks = 1024, kMostBlocks = 4096, kChunksEach = 4;
 // Gradients' bytes from which the norm alone reads past the caches: they do not
-// fit the last-level one anyway (2^28 fp32: 206 us with plain loads, 182 with
-// these; 2^26 bf16: 27 and 30).  A clipping's first pass leaves there what it
+// fit the last-level one anyway (2^28 fp32: 188 us with plain loads, 165 with
+// these; 2^27 bf16 of one set again and again 51 and 55, 2^26 27 and 29.5, which of
+// three sets in turn are 30 and 28).  A clipping's first pass leaves there what it
 // can for the second.
 constexpr int64_t kStreamNorm = 256 << 20;
 // LDS that a workgroup of either pass takes, though it needs little of it, so
@@ -81,8 +86,8 @@ __device__ __forceinline__ int first_chunk(const Table &t, int b) { return (int)
 // The workgroup whose chunks this one scales: eight at a time in the opposite
 // order, where more run than are resident, and on the same of the eight XCDs
 // (workgroups go to them in turn), whose L2 still holds them after the first
-// pass.  2^23 bf16: 18.4 us in the plain opposite order, 15.7 so; 2^28: 389 and
-// 387; in the first pass's own order 15.5 and 424.
+// pass.  2^23 bf16: 19.1 us in the plain opposite order, 17.3 so, 17.0 in the first
+// pass's own order; 2^25 fp32 76.6, 72.4 and 77.5; 2^28 fp32 586, 586 and 603.
 __device__ __forceinline__ int opposite() {
   const uint32_t n = gridDim.x, b = blockIdx.x;
   return (int)(n % 8 ? b : (n - 8 - (b & ~7u)) | (b & 7u));
@@ -197,8 +202,8 @@ __device__ __forceinline__ Scale scale_of(double ratio) {
 // A lane's access is 16 bytes of the output, where the chunks begin with a
 // line: into a flat vector, in which tensors begin anywhere, whole lines are
 // written.  Nontemporal stores leave the last-level cache to the gradients that
-// the pass is still to read (2^25 fp32, both passes: 85 us with plain stores, 64
-// with these; 2^23: 23 and 20).
+// the pass is still to read (2^25 fp32, both passes: 95 us with plain stores, 72
+// with these; 2^23: 22.4 and 21.1; 2^28 bf16 into fp32: 570 and 408).
 template <typename T, typename U>
 __device__ __forceinline__ void scale_chunk(const Entry &e, int64_t chunk, int c, Scale s) {
   constexpr int V = Chunk<U>::kElems;

@@ -14,23 +14,31 @@
 //
 // A row lies in the registers of 16 lanes (four rows per wave) up to 256
 // experts, of a whole wave beyond, N values each, so that a reduction takes
-// four lane-rotating instructions (and reads of four lanes into scalar registers
-// for a whole wave).  Logits are compared as unsigned keys in the order of the
-// floats, -0 as +0, NaN above everything.  A 16-bit logit's key and its
-// expert's number make one word, all different, so that a maximum finds the
-// lowest of equal ones by itself; of fp32 logits the upper part of the key does
-// (select), or the lanes that hold the maximum are counted.
+// four lane-rotating instructions (for a whole wave two more, which join the rows
+// of 16 lanes, and a read of the last lane into a scalar register).
+//
+// Logits are compared as unsigned keys in the order of the floats, -0 as +0, NaN
+// above everything.  A 16-bit logit's key and its expert's number make one word,
+// all different, so that a maximum finds the lowest of equal ones by itself; of
+// fp32 logits the upper part of the key does (select), or the lanes that hold the
+// maximum are counted.
 //
 // The softmax is in fp32 whatever the logits' type; exponentials are exp2 of
 // the product with log2 e, off by some 2 |z - m| 2^-24 relative to themselves;
 // weights below fp32's normal numbers become 0.
 //
-// Bound by instructions for many tokens (k rounds of a maximum).  32768 tokens,
-// k = 8: 64 experts, bf16: 4.3 us, where reading and writing would take 1.2
-// (4.9 with a maximum over all values of a lane in every round, 6.6 with equal
-// keys found by a second reduction); 256 experts: bf16 9.5 us (11.7, reading 3.2),
-// fp32 12.0 (15.3, reading 6.3).  The gradient of 16384 tokens, 256 experts, fp32:
-// 8.6 us (6.8; 11.5 with the k terms compared with every expert).
+// Bound by instructions for many tokens (the lanes' sorts and k rounds of a
+// maximum).  32768 tokens, k = 8: 64 experts, bf16: 4.3 us, where reading and
+// writing would take 1.2 (4.9 with a maximum over all values of a lane in every
+// round, 6.6 with equal keys found by a second reduction); 256 experts: bf16 9.4 us
+// (11.7, reading 3.2), fp32 11.8 (15.3, reading 6.3).  Of these the vector
+// instructions alone, 213, 516 and 492 a wave, 8 waves a SIMD, four clocks each
+// at 2.4 GHz, are 2.8, 6.9 and 6.6 us; of 512 experts fp32 (20.1 us, reading
+// 12.7), 346 a wave, 32 waves a SIMD, 18.5.  1024 experts: bf16 27, fp32 35 us.
+//
+// The gradient of 16384 tokens, 256 experts, fp32: 8.4 us over all experts (11.5
+// with the k terms compared with every expert), where reading and writing would
+// take 6.5, and 6.5 over the chosen ones, which reads k logits of a row.
 #include <cmath>
 #include <utility>
 
@@ -44,7 +52,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxExperts = 1024, kMaxK = 16;
 
 // Keys in the order of the logits; the key of a masked or absent expert is at
-// most kMasked.  value_of gives a key's logit.
+// most kMasked.  value gives a key's logit.
 template <typename T>
 struct Key;
 
@@ -142,9 +150,8 @@ __device__ __forceinline__ void sort_down(uint32_t (&v)[N], std::index_sequence<
 
 // The `rounds` <= R largest of each group's keys, all different but for 0:
 // lane j gets the j-th, every lane the first (`most`), the last one, and the one
-// before it.  Each
-// lane sorts its own, so that a round looks at the lanes' first ones alone; of
-// what is behind them only as many as there are rounds left move up.
+// before it.  Each lane sorts its own, so that a round looks at the lanes' first
+// ones alone; of what is behind them only as many as there are rounds left move up.
 template <int G, int N, int R, int J = 0>
 __device__ __forceinline__ void take_rounds(uint32_t (&key)[N], int l, int rounds, uint32_t &mine, uint32_t &most, uint32_t &last,
                                             uint32_t &before) {

@@ -92,10 +92,15 @@ __device__ __forceinline__ void store(T *p, typename Chunk<T>::vec v) {
 }
 
 // Whether a group of lanes (8, 16 or 32, a chunk each) takes a token, where a
-// wave would leave most of its lanes idle (us with a wave and with a group: two
-// rows of 64 bf16 combined, 32768 tokens 10.8 and 3.8, 8000 3.9 and 2.6, 4000 3.1
-// and 2.6, their gradient 18.7 and 6.1, 5.2 and 3.5, 3.5 and 3.4; eight rows of
-// 256, 32768 tokens: 26.4 and 33.1, four 16.2 and 14.8).
+// wave would leave most of its lanes idle.  One rule for the three operators, from
+// where the gradient's two forms cross (us with a wave and with a group, bf16;
+// two rows of 64: 32768 tokens 18.7 and 6.1, 6000 4.0 and 3.3, 4000 3.1 and 3.2;
+// eight of 128: 6000 9.9 and 9.2, 4000 7.4 and 8.2; four of 256: 8000 9.2 and 9.0,
+// 6000 7.8 and 7.7).  The combination's cross earlier (two of 64: 32768 tokens
+// 10.8 and 3.8, 6000 3.3 and 2.4, 3000 2.6 and 2.35, 1000 2.25 and 2.3; eight of
+// 128: 3000 4.0 and 4.2), the copies of the dispatch near it (8000 tokens, eight
+// of 64 11.4 and 10.5, four of 256 11.2 and 11.8).  Eight rows of 256 combined for
+// 32768 tokens: 26.4 and 33.1, four 16.2 and 14.8.
 inline bool narrow_rows(int64_t chunks, int64_t n_tokens, int32_t k) {
   return chunks <= (k <= 4 ? 32 : 16) && n_tokens >= 6144;
 }

@@ -292,8 +292,9 @@ def moe_dispatch_grad(grad_rows, pos, *, out=None, stream=None):
 def moe_combine_grad(grad_y, rows, pos, weights, *, grad_rows=None, grad_weights=None, stream=None):
     """(grad_rows, grad_weights) of the combination: grad_rows[pos[t, j]] =
     weights[t, j] * grad_y[t], grad_weights[t, j] = <grad_y[t],
-    rows[pos[t, j]]>.  Rows that no slot names are left as they were (zeros in
-    a grad_rows that the call allocates)."""
+    rows[pos[t, j]]>.  Slots have different rows, as the dispatch gives them;
+    rows that no slot names are left as they were (zeros in a grad_rows that
+    the call allocates, which costs a pass over it)."""
     name = "moe_combine_grad"
     device, size, shape = grad_y.get_device(), grad_y.shape, rows.shape
     if device < 0 or device != _device() or len(size) != 2:
@@ -347,10 +348,11 @@ class GradSet:
     other (float32, or the type of all of them: the gradient buffer of an
     AdamW plan), or a tensor for each.  Like a plan its program, the set keeps
     a table of the tensors on the device, and their memory: a gradient that is
-    allocated anew needs a new set.  A gradient named twice counts twice in the
+    allocated anew (as torch's zero_grad() lets them be) needs a new set, the
+    old one goes on with the old memory.  A gradient named twice counts twice in the
     norm; a set whose outputs overlap (that one in place, say) is not clipped.
-    Making one copies the table (it waits for the copy and cannot be captured);
-    the calls can be.  A set may be dropped while a call of it is under way, on
+    Making one copies the table (it waits for the copy, some 60 us of the host
+    for 24 tensors, 470 for 290, and cannot be captured); the calls can be.  A set may be dropped while a call of it is under way, on
     whatever stream: its memory is used again only behind that stream's work.
     A stream given by its handle has to exist until the set is gone, and a set
     whose calls were captured has to be kept as long as the graph."""
@@ -448,8 +450,9 @@ class GradSet:
 
     def clip(self, max_norm, norm=None, workspace=None, stream=None):
         """Writes grads * min(1, max_norm / (norm + 1e-6)) to the outputs and
-        returns the norm before clipping.  A norm that is not finite (in
-        float32) scales by 1."""
+        returns the norm before clipping.  A norm that is not finite in
+        float32, as it is returned, scales by 1, also where only float32 does
+        not hold it: gradients beside an infinite norm are as they were."""
         norm, workspace, size, handle = self._buffers("grad_clip", norm, workspace, stream)
         address, table = self._args
         status = bfs._lib.bfs_call(_CLIP(6, 7, address, table, max_norm, norm.data_ptr(), workspace.data_ptr(), size, handle))
