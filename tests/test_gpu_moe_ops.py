@@ -665,3 +665,30 @@ def test_dispatch_sums_of_many_groups(t, k, e, h, drop):
     assert t * k > 8192 and 1024 <= groups * e <= 4096 and groups > 8 * (512 // e)
     for skew in (False, True):
         _check_dispatch(t, k, e, h, torch.bfloat16, 1, drop, skew)
+
+
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("e,k", [(40, 3), (64, 8), (200, 2), (256, 16), (600, 6)])
+def test_not_a_number_and_infinity(e, k, dtype, renorm):
+    """In every form of the router: NaN of either sign before +inf before the
+    rest, equal ones by index; all weights of such a token are NaN, and its
+    gradients over all experts; others as without it."""
+    z = _normal(e, (9, e), dtype)
+    z[1] = float("-inf")                               # a token without experts between them
+    clean = bfsp.moe_route(z, k, renormalize=renorm)
+    dw = _normal(k, (9, k))
+    clean_dz = bfsp.moe_route_grad(z, clean[0], dw, renormalize=renorm)
+    z[2, e - 1], z[2, 3], z[2, 5] = float("nan"), float("inf"), -float("nan")
+    z[4, 7] = z[4, 6] = float("inf")
+    z[6] = float("nan")
+    experts, weights = bfsp.moe_route(z, k, renormalize=renorm)
+    dz = bfsp.moe_route_grad(z, experts, dw, renormalize=renorm)
+    first = experts.cpu().numpy()
+    assert np.array_equal(first[2, :3], [5, e - 1, 3][:k]) and np.array_equal(first[4, :2], [6, 7])
+    assert np.array_equal(first[6], np.arange(k)) and (first[1] == -1).all() and (weights[1] == 0).all()
+    bad, keep = [2, 4, 6], [0, 1, 3, 5, 7, 8]
+    assert weights[bad].isnan().all()
+    taking_part = dz[bad].gather(1, experts[bad].long()) if renorm else dz[bad]
+    assert taking_part.isnan().all()
+    assert torch.equal(experts[keep], clean[0][keep]) and torch.equal(weights[keep], clean[1][keep]) and torch.equal(dz[keep], clean_dz[keep])
