@@ -415,8 +415,8 @@ class GradSet:
         each stream, it holds until the memory goes back."""
         if stream is None:
             stream = torch.cuda.current_stream()
-        elif isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream)
+        elif isinstance(stream, int):                  # (no handle of torch's wrapper: 0, the default stream)
+            stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
         for t in self._keep:
             t.record_stream(stream)
         self._used_on.add(handle)

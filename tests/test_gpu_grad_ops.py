@@ -243,3 +243,21 @@ def test_set_dropped_while_another_stream_uses_it(call):
     for o, g, w in zip(out.split([g.numel() for g in grads]), grads, want):
         assert bool(((o.double() - w).abs() <= w.abs() * 4 * U).all())
     assert all((z == 0).all() for z in zeros[:5])
+
+
+def test_set_dropped_while_the_default_stream_uses_it():
+    """A set made on a stream of its own, its call on the default stream."""
+    grads = _grads(13, [9001, 70_001], [torch.float32])
+    want = [g.double() * min(1.0, 0.25 / (_norm64(grads) + 1e-6)) for g in grads]
+    out, norm = torch.zeros(79_002, device="cuda"), torch.zeros((), device="cuda")
+    workspace = torch.empty(GradSet(grads).workspace_bytes, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    with torch.cuda.stream(torch.cuda.Stream()):
+        bfsp.grad_clip(grads, 0.25, out=out, norm=norm, workspace=workspace, stream=torch.cuda.default_stream().cuda_stream)
+        zeros = [torch.zeros(n, dtype=torch.uint8, device="cuda") for n in [512, 1024, 2048, 4096, 8192] * 40]
+    torch.cuda.synchronize()
+    _check_norm(norm, grads)
+    for o, w in zip(out.split([g.numel() for g in grads]), want):
+        assert bool(((o.double() - w).abs() <= w.abs() * 4 * U).all())
+    assert all((z == 0).all() for z in zeros[:5])

@@ -305,3 +305,23 @@ def test_ids_that_are_no_matrix(shape, monkeypatch):
         with pytest.raises(BfsError) as e:
             call()
         assert e.value.status == bfs.E_INVALID
+
+
+def test_set_of_gradients_used_on_the_default_stream(monkeypatch):
+    """Of a set made on a stream of its own, called by the default stream's
+    handle, which is 0: torch's wrapper of handles would make another stream of
+    that.  On the host, with the launch left out."""
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+
+    from paper_2608_13757_amd import ops
+    real, events = bfs.lib(), []
+    monkeypatch.setattr(ops, "_device", lambda: 0)
+    monkeypatch.setattr(ops, "_raw_stream", lambda device: 5)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: events.append(s), raising=False)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: "external")
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda: "default")
+    monkeypatch.setattr(bfs, "_lib", SimpleNamespace(bfs_grad_table=real.bfs_grad_table,
+                                                     bfs_call=lambda words: events.append("call") or 0))
+    ops.grad_norm([_on_device(torch, 50)], norm=_on_device(torch, ()), workspace=_on_device(torch, 64, dtype=torch.float64), stream=0)
+    assert events == ["default"] * 3 + ["call"]         # the gradient twice (it is its own output), the table
